@@ -411,6 +411,119 @@ int selective_state_update(void* state, const void* x, const void* delta, const 
                            int32_t delta_softplus, void* y, corey_dtype dt, int64_t B, int64_t D, int64_t N,
                            void* hip_stream);
 
+/* -------------------------------------------------------------------------------------------------------
+ * Packed batches -- the layer's recurrent steps on batches without padding, as servers and trainers form them: the tokens of
+ * S sequences of any lengths one after another in T rows, [T, D], and the sequences' states in pools, found by slot.  The
+ * operators are those of causal_conv1d_silu_fwd, selective_scan_fwd and selective_state_update (Method, Preliminaries) for every
+ * sequence by itself, and their gradients.
+ *   - Activations (x, u, delta, z, y, ...) are token-major, as the projections around them write and read them: row t holds
+ *     token t's D channels (or N states, B and C) without gaps, and rows lie `..._stride` elements apart (>= D, or N; < 2^31).
+ *     Any alignment is taken.  An output may not overlap an input or another output (an output that IS an input is refused).
+ *   - Rows behind the last sequence (T may be more than the lengths add up to) are neither read nor written.
+ *   - slots, slots_out   DEVICE int32[S]: sequence s begins from pool entry slots[s] and leaves its state in slots_out[s].
+ *     slots NULL, or an entry outside [0, n_slots) (-1, say): it begins from zero.  slots_out NULL: the same as slots; an entry
+ *     outside: the state is not kept.  slots[s] == slots_out[s] moves a state on in place; different ones leave the old state as
+ *     it is (a prompt's state from which several continuations begin).  No slot may be written for two sequences of a call, or
+ *     written for one and read for another: which state is read or kept would be undefined.  A sequence without tokens
+ *     leaves both its slots as they are.
+ *   - Arithmetic, sums and scan states in binary32; results are rounded once to `dt`.
+ * ----------------------------------------------------------------------------------------------------- */
+#define COREY_PACK_BLOCK 16               /* tokens of the small pieces                                   */
+#define COREY_PACK_MAX_TILE 2048
+#define COREY_PACK_MAX_SEQS (1 << 20)     /* S                                                            */
+#define COREY_PACK_MAX_CHANNELS (1 << 20) /* D of the packed operators                                    */
+#define COREY_PACK_MAX_STATE 128          /* N of corey_scan_packed and its gradients                     */
+
+/* The index of a packed batch; filled by corey_pack_plan, read by the calls below.  `table` stays the caller's memory. */
+typedef struct {
+    void*   table;                        /* DEVICE */
+    size_t  bytes;
+    int64_t S, T;
+    int32_t tile, reserved;
+} corey_pack;
+
+/* corey_pack_plan -- builds the index on the GPU from the sequences' lengths, without a host round trip.
+ *   lengths     DEVICE int32[S], 1 <= S <= COREY_PACK_MAX_SEQS.  Lengths below 0 count as 0; sequences that do not fit into T rows
+ *               are cut off there.       T: rows of the batch's tensors, 1 <= T < 2^31.
+ *   tile        power of two in [COREY_PACK_BLOCK, COREY_PACK_MAX_TILE]: tokens of a sequence that the scan walks in one go
+ *               (corey_pack_tile gives a good one).  The results do not depend on it beyond reassociation.
+ *   table       DEVICE, corey_pack_bytes(S, T, tile) bytes, 16-byte aligned.  int32 words: a head of 16 (words 4 .. 7: tokens, tiles,
+ *               blocks in use, sequences of more than one tile); starts[S + 1], the row each sequence begins at and the end;
+ *               seq[T], the sequence of each row (-1 behind the last); tiles[T / tile + min(S, T)][4] and
+ *               blocks[T / 16 + min(S, T)][4], the pieces of at most `tile` and 16 tokens of one sequence: sequence, first row,
+ *               tokens, bits (1 the sequence's first piece, 2 its last), and -1, 0, 0, 0 behind the used ones; then what only
+ *               the operators read.  Every part begins at a multiple of four words.
+ *   pack        HOST, filled.
+ * The calls that take `pack` must be ordered behind this one on the GPU, and the table must stay as it is while they run.  They
+ * check on the GPU that it holds an index of the sizes `pack` names, and do nothing if it does not.
+ * Errors: COREY_ENULL, COREY_ESHAPE (S, T), COREY_EINVAL (tile), COREY_EWORKSPACE, COREY_EHIP; *pack is then left as it was. */
+int corey_pack_plan(const int32_t* lengths, int64_t S, int64_t T, int32_t tile, void* table, size_t table_bytes, corey_pack* pack,
+                    void* hip_stream);
+/* Bytes of table corey_pack_plan needs (0 if the arguments are invalid). */
+size_t corey_pack_bytes(int64_t S, int64_t T, int32_t tile);
+/* A good tile for T rows in S sequences through layers of D channels and N states: as long as enough tiles run side by side; for
+ * backward != 0 the one corey_scan_packed_bwd works best with (forward calls take it too).  0 if the arguments are invalid. */
+int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward);
+
+/* corey_conv_packed -- causal_conv1d_silu_fwd on a packed batch: u = v sigmoid(v), v[t] = bias + sum_k weight[k] x[t - (W-1) + k].
+ *   x, u        DEVICE rows of D in `dt`.     weight DEVICE float[D, W], 1 <= W <= COREY_MAX_CONV.   bias DEVICE float[D] or NULL.
+ *   state       DEVICE [n_slots, D, W-1] in `dt`: each entry the last W-1 inputs, oldest first.  NULL without slots.
+ * One token per sequence (generation) is a batch like any other.
+ * Errors: COREY_ENULL, COREY_EINVAL (dtype, W, u == x, a pack not filled by corey_pack_plan), COREY_ESHAPE, COREY_EWORKSPACE (table), COREY_EHIP. */
+int corey_conv_packed(const void* x, int64_t x_stride, const float* weight, const float* bias, void* state, int64_t n_slots,
+                      const int32_t* slots, const int32_t* slots_out, const corey_pack* pack, void* u, int64_t u_stride, corey_dtype dt,
+                      int64_t D, int32_t W, void* hip_stream);
+
+/* corey_conv_packed_bwd -- gradients of corey_conv_packed for sequences that began from zero (no slots), as packed training has them:
+ * with dv = du silu'(v),  dx[t] = sum_k weight[k] dv[t + (W-1) - k] inside the sequence, dweight[k] = sum_t dv[t] x[t - (W-1) + k],
+ * dbias = sum_t dv[t].  v is formed again from x.
+ *   du, dx      DEVICE rows of D in `dt`.     dweight DEVICE float[D, W].   dbias DEVICE float[D] or NULL.
+ *   workspace   DEVICE, corey_conv_packed_bwd_workspace() bytes, 4-byte aligned; scratch.
+ * The sums run in a fixed order: equal calls give equal bits. */
+int corey_conv_packed_bwd(const void* x, int64_t x_stride, const float* weight, const float* bias, const void* du, int64_t du_stride,
+                          const corey_pack* pack, void* dx, int64_t dx_stride, float* dweight, float* dbias, corey_dtype dt, int64_t D,
+                          int32_t W, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t corey_conv_packed_bwd_workspace(const corey_pack* pack, int64_t D, int32_t W);
+
+/* corey_scan_packed -- selective_scan_fwd on a packed batch.  Formulas, A, Dv, delta_bias, delta_softplus and z as there (z, Dv and
+ * delta_bias may be NULL; strides of absent tensors are not read).
+ *   u, delta, z, y   DEVICE rows of D in `dt`.    Bm, Cm: DEVICE rows of N in `dt`, 1 <= N <= COREY_PACK_MAX_STATE.
+ *   state       DEVICE float[n_slots, D, N]; NULL without slots.
+ *   workspace   DEVICE, corey_scan_packed_workspace() bytes, 16-byte aligned; scratch.
+ * Errors: as corey_conv_packed; COREY_EUNSUPPORTED for a larger N; COREY_EWORKSPACE. */
+int corey_scan_packed(const void* u, int64_t u_stride, const void* delta, int64_t delta_stride, const float* A, const void* Bm,
+                      int64_t B_stride, const void* Cm, int64_t C_stride, const float* Dv, const void* z, int64_t z_stride,
+                      const float* delta_bias, int delta_softplus, float* state, int64_t n_slots, const int32_t* slots,
+                      const int32_t* slots_out, const corey_pack* pack, void* y, int64_t y_stride, corey_dtype dt, int64_t D, int64_t N,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t corey_scan_packed_workspace(const corey_pack* pack, int64_t D, int64_t N);
+
+/* corey_scan_packed_step -- selective_state_update with the states in a pool: one token of each of S sequences.
+ *   x, delta, z, y   DEVICE S rows of D in `dt`.   Bt, Ct: DEVICE S rows of N in `dt`, 1 <= N <= COREY_MAX_STATE.   S*D < 2^25.
+ *   state, slots     required. */
+int corey_scan_packed_step(float* state, int64_t n_slots, const int32_t* slots, const int32_t* slots_out, const void* x, int64_t x_stride,
+                           const void* delta, int64_t delta_stride, const float* A, const void* Bt, int64_t B_stride, const void* Ct,
+                           int64_t C_stride, const float* Dv, const void* z, int64_t z_stride, const float* delta_bias, int delta_softplus,
+                           void* y, int64_t y_stride, corey_dtype dt, int64_t S, int64_t D, int64_t N, void* hip_stream);
+
+/* corey_scan_packed_bwd -- gradients of corey_scan_packed for sequences that began from zero (no slots), from dy and the inputs alone
+ * (the states are formed again).  With ds = dy silu(z), a_t = exp(dl_t A), g_t = ds_t C_t + a_{t+1} g_{t+1} inside the sequence:
+ *     dC_t = sum_d ds_t h_t       dB_t = sum_d g_t dl_t u_t        dz = dy s silu'(z), s the read-out before the gate
+ *     du = Dv ds + dl sum_n g B   ddl = sum_n g (u B + A a_t h_{t-1})      ddelta = ddl sigmoid(delta + bias) (or ddl without softplus)
+ *     dA = sum_t g dl a_t h_{t-1}     dDv = sum_t ds u      ddelta_bias = sum_t ddelta
+ *   du, ddelta, dz   DEVICE rows of D in `dt` (dz: required iff z is).   dB, dC: DEVICE rows of N in `dt`.
+ *   dA               DEVICE float[D, N].   dDv, ddelta_bias: DEVICE float[D] or NULL.
+ *   pack             tile <= 64, and <= 32 for N > 64 (COREY_EUNSUPPORTED otherwise; corey_pack_tile with backward gives it).
+ *   workspace        DEVICE, corey_scan_packed_bwd_workspace() bytes, 16-byte aligned; scratch.
+ * The sums over channels and tokens run in a fixed order: equal calls give equal bits. */
+int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void* delta, int64_t delta_stride, const float* A, const void* Bm,
+                          int64_t B_stride, const void* Cm, int64_t C_stride, const float* Dv, const void* z, int64_t z_stride,
+                          const float* delta_bias, int delta_softplus, const void* dy, int64_t dy_stride, const corey_pack* pack, void* du,
+                          int64_t du_stride, void* ddelta, int64_t ddelta_stride, float* dA, void* dB, int64_t dB_stride, void* dC,
+                          int64_t dC_stride, float* dDv, void* dz, int64_t dz_stride, float* ddelta_bias, corey_dtype dt, int64_t D,
+                          int64_t N, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t corey_scan_packed_bwd_workspace(const corey_pack* pack, int64_t D, int64_t N);
+
 #ifdef __cplusplus
 }
 #endif

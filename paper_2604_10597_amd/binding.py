@@ -22,7 +22,10 @@ STATUS = {0: "COREY_OK", 1: "COREY_EINVAL", 2: "COREY_ENULL", 3: "COREY_ESHAPE",
 EXPORTS = ("corey_entropy_hist", "corey_entropy_hist_static", "corey_entropy_hist_workspace", "corey_pattern_table_workspace",
            "corey_entropy_hist_onesweep", "corey_entropy_hist_from_table", "corey_policy_default", "corey_select_chunk",
            "corey_select_chunk_device", "corey_route_device", "corey_route_device_deferred", "selective_scan_fwd_routed", "corey_ema_update", "causal_conv1d_silu_fwd", "selective_state_update",
-           "selective_scan_fwd", "selective_scan_fwd_workspace", "selective_scan_fwd_plan", "selective_scan_fwd_plan_steps", "selective_scan_fwd_plan_split", "corey_last_error", "corey_version")
+           "selective_scan_fwd", "selective_scan_fwd_workspace", "selective_scan_fwd_plan", "selective_scan_fwd_plan_steps", "selective_scan_fwd_plan_split", "corey_last_error", "corey_version",
+           "corey_pack_plan", "corey_pack_bytes", "corey_pack_tile", "corey_conv_packed", "corey_conv_packed_bwd",
+           "corey_conv_packed_bwd_workspace", "corey_scan_packed", "corey_scan_packed_workspace", "corey_scan_packed_step",
+           "corey_scan_packed_bwd", "corey_scan_packed_bwd_workspace")
 
 
 class CoreyError(RuntimeError):
@@ -42,6 +45,42 @@ class Policy(ctypes.Structure):
 class DeferredRoute(ctypes.Structure):
     """corey_deferred_route: opaque, filled by corey_route_device_deferred, consumed by selective_scan_fwd_routed"""
     _fields_ = [("opaque", ctypes.c_uint64 * 40)]
+
+
+class Pack(ctypes.Structure):
+    """corey_pack: the index of a packed batch, as corey_pack_plan returns it.  S sequences in T rows, pieces of `tile` tokens;
+    `table` is the int32 GPU tensor that holds it.  The index is also the caller's to read (GPU tensors, views of the table):
+      starts [S + 1]  the row each sequence begins at, and the end of the last: starts[1:] - 1 are the sequences' last rows
+      seq [T]         the sequence of each row, -1 behind the last
+      tiles, blocks   [., 4] the pieces of at most `tile` and 16 tokens: sequence, first row, tokens, bits (1 first, 2 last piece of its
+                      sequence); -1, 0, 0, 0 behind the used ones"""
+    _fields_ = [("_table", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("S", ctypes.c_int64), ("T", ctypes.c_int64),
+                ("tile", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+    def _at(self, part: int) -> int:
+        """The word a part begins at: starts, seq, tiles, blocks (include/corey.h)."""
+        up = lambda n: -(-n // 4) * 4
+        sizes = (16, up(self.S + 1), up(self.T), 4 * self._pieces(self.tile))
+        return sum(sizes[:part + 1])
+
+    def _pieces(self, size: int) -> int:
+        return self.T // size + min(self.S, self.T)
+
+    @property
+    def starts(self) -> torch.Tensor:
+        return self.table.as_strided((self.S + 1,), (1,), self.table.storage_offset() + self._at(0))
+
+    @property
+    def seq(self) -> torch.Tensor:
+        return self.table.as_strided((self.T,), (1,), self.table.storage_offset() + self._at(1))
+
+    @property
+    def tiles(self) -> torch.Tensor:
+        return self.table.as_strided((self._pieces(self.tile), 4), (4, 1), self.table.storage_offset() + self._at(2))
+
+    @property
+    def blocks(self) -> torch.Tensor:
+        return self.table.as_strided((self._pieces(16), 4), (4, 1), self.table.storage_offset() + self._at(3))
 
 
 _lib = None
@@ -102,6 +141,32 @@ def lib() -> ctypes.CDLL:
         L.selective_scan_fwd_plan_split.argtypes = [i64, i64, i64, i32]
         L.selective_scan_fwd_workspace.restype = ctypes.c_size_t
         L.selective_scan_fwd_workspace.argtypes = [i64, i64, i64]
+        sz, pk = ctypes.c_size_t, ctypes.POINTER(Pack)
+        L.corey_pack_plan.restype = ctypes.c_int
+        L.corey_pack_plan.argtypes = [vp, i64, i64, i32, vp, sz, pk, vp]
+        L.corey_pack_bytes.restype = sz
+        L.corey_pack_bytes.argtypes = [i64, i64, i32]
+        L.corey_pack_tile.restype = i32
+        L.corey_pack_tile.argtypes = [i64, i64, i64, i64, ctypes.c_int]
+        L.corey_conv_packed.restype = ctypes.c_int
+        L.corey_conv_packed.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, pk, vp, i64, ctypes.c_int, i64, i32, vp]
+        L.corey_conv_packed_bwd.restype = ctypes.c_int
+        L.corey_conv_packed_bwd.argtypes = [vp, i64, vp, vp, vp, i64, pk, vp, i64, vp, vp, ctypes.c_int, i64, i32, vp, sz, vp]
+        L.corey_conv_packed_bwd_workspace.restype = sz
+        L.corey_conv_packed_bwd_workspace.argtypes = [pk, i64, i32]
+        L.corey_scan_packed.restype = ctypes.c_int
+        L.corey_scan_packed.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, ctypes.c_int, vp, i64, vp, vp, pk, vp, i64,
+                                        ctypes.c_int, i64, i64, vp, sz, vp]
+        L.corey_scan_packed_workspace.restype = sz
+        L.corey_scan_packed_workspace.argtypes = [pk, i64, i64]
+        L.corey_scan_packed_step.restype = ctypes.c_int
+        L.corey_scan_packed_step.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, ctypes.c_int, vp, i64,
+                                             ctypes.c_int, i64, i64, i64, vp]
+        L.corey_scan_packed_bwd.restype = ctypes.c_int
+        L.corey_scan_packed_bwd.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, ctypes.c_int, vp, i64, pk, vp, i64, vp, i64,
+                                            vp, vp, i64, vp, i64, vp, vp, i64, vp, ctypes.c_int, i64, i64, vp, sz, vp]
+        L.corey_scan_packed_bwd_workspace.restype = sz
+        L.corey_scan_packed_bwd_workspace.argtypes = [pk, i64, i64]
         L.corey_last_error.restype = ctypes.c_char_p
         L.corey_version.restype = ctypes.c_char_p
         _lib = L
@@ -291,3 +356,52 @@ def selective_scan_fwd(u, delta, A, Bm, Cm, Dv=None, z=None, delta_bias=None, de
     `route`: the ticket of corey_route_device_deferred; the call is then selective_scan_fwd_routed (no chunks_dev)."""
     return (_ext or _native()).selective_scan_fwd(u, delta, A, Bm, Cm, Dv, z, delta_bias, delta_softplus, h0, seqlens, chunk, chunks_dev, y,
                                                   last_state, workspace, general_a, route, whole_rows)
+
+
+def corey_pack_tile(S: int, T: int, D: int, N: int = 16, backward: bool = False) -> int:
+    """A good `tile` for T rows in S sequences through layers of D channels and N states (backward: for corey_scan_packed_bwd)."""
+    return int(lib().corey_pack_tile(S, T, D, N, 1 if backward else 0))
+
+
+def corey_pack_plan(lengths: torch.Tensor, T: int, tile: int, table: torch.Tensor | None = None) -> Pack:
+    """The index of a packed batch of T rows from int32 lengths [S] on the GPU, without a host round trip.  One index serves every
+    layer and call that the batch goes through.  `table`: int32 GPU tensor of corey_pack_bytes / 4 words (allocated here if omitted)."""
+    p = Pack()
+    p.table = (_ext or _native()).corey_pack_plan(lengths, T, tile, table, p)
+    return p
+
+
+def corey_conv_packed(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None, pack: Pack, state: torch.Tensor | None = None,
+                      slots: torch.Tensor | None = None, slots_out: torch.Tensor | None = None, u: torch.Tensor | None = None) -> torch.Tensor:
+    """causal_conv1d_silu_fwd on a packed batch: x [T, D] (rows any distance apart), weight float32 [D, W], bias float32 [D] or None;
+    state [slots, D, W - 1] in x's type, slots and slots_out int32 [S] as in include/corey.h.  Returns u [T, D]; of an u allocated here
+    the rows behind the last sequence hold whatever the memory held."""
+    return (_ext or _native()).corey_conv_packed(x, weight, bias, pack, state, slots, slots_out, u)
+
+
+def corey_conv_packed_bwd(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None, du: torch.Tensor, pack: Pack,
+                          workspace: torch.Tensor | None = None):
+    """Gradients of corey_conv_packed without slots: (dx [T, D], dweight float32 [D, W], dbias float32 [D])."""
+    return (_ext or _native()).corey_conv_packed_bwd(x, weight, bias, du, pack, workspace)
+
+
+def corey_scan_packed(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, Cm: torch.Tensor, pack: Pack, Dv=None, z=None,
+                      delta_bias=None, delta_softplus: bool = True, state=None, slots=None, slots_out=None, y=None, workspace=None) -> torch.Tensor:
+    """selective_scan_fwd on a packed batch: u, delta, z [T, D], Bm, Cm [T, N] (rows any distance apart), A float32 [D, N]; state float32
+    [slots, D, N], slots and slots_out int32 [S] as in include/corey.h.  Returns y [T, D]."""
+    return (_ext or _native()).corey_scan_packed(u, delta, A, Bm, Cm, pack, Dv, z, delta_bias, delta_softplus, state, slots, slots_out, y, workspace)
+
+
+def corey_scan_packed_step(state: torch.Tensor, slots: torch.Tensor, x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bt: torch.Tensor,
+                           Ct: torch.Tensor, Dv=None, z=None, delta_bias=None, delta_softplus: bool = True, slots_out=None, y=None) -> torch.Tensor:
+    """One token of each of S sequences, states by slot: x, delta, z [S, D], Bt, Ct [S, N]; returns y [S, D]."""
+    return (_ext or _native()).corey_scan_packed_step(state, slots, x, delta, A, Bt, Ct, Dv, z, delta_bias, delta_softplus, slots_out, y)
+
+
+def corey_scan_packed_bwd(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, Cm: torch.Tensor, pack: Pack,
+                          dy: torch.Tensor, Dv=None, z=None, delta_bias=None, delta_softplus: bool = True, out: dict | None = None,
+                          workspace=None) -> dict:
+    """Gradients of corey_scan_packed without slots, from dy and its inputs: dict(du, ddelta, dA, dB, dC and, where the input was
+    given, dD, dz, ddelta_bias).  `pack`: of tile 64 at most, 32 for N > 64 (corey_pack_tile with backward).  `out`: a dict whose tensors are
+    written (missing ones are allocated)."""
+    return (_ext or _native()).corey_scan_packed_bwd(u, delta, A, Bm, Cm, pack, dy, Dv, z, delta_bias, delta_softplus, out, workspace)

@@ -14,6 +14,7 @@ LIB = os.path.join(HERE, "libcorey.so")
 NATIVE = os.path.join(HERE, "_native.so")          # Python extension: marshals torch tensors into libcorey
 # the scan's kernels in several translation units: they compile side by side (the longest first)
 SOURCES = [f"corey_scan_any_{t}_w{w}.hip" for t in ("bf16", "f16", "f32") for w in (3, 4)] + [
+    "corey_packed_scan_bwd.hip", "corey_packed_scan.hip", "corey_packed_conv.hip", "corey_packed_plan.hip",
     "corey_scan_bf16.hip", "corey_scan_f16.hip", "corey_scan_f32.hip", "corey_conv.hip", "corey_entropy.hip", "corey_table.hip",
     "corey_decode.hip", "corey_scan.hip", "corey_host.cpp"]
 

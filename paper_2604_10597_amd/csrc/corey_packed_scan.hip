@@ -1,0 +1,457 @@
+// corey_scan_packed and corey_scan_packed_step: the selective scan on packed batches [T, D], states by slot.
+//
+//     dl = softplus(delta + bias);  h[n] <- exp(dl A[n]) h[n] + dl B[n] u;  y = (sum_n C[n] h[n] + D u) silu(z)
+//
+// Neighbouring channels lie side by side in memory, so a lane is a pair of channels and walks the tokens one after another: B and C
+// of a token are the same for the whole wave (one LDS word read by all lanes), the states stay in registers, and nothing is
+// exchanged between lanes.  Per token, channel and state that is one exponential and four plain instructions; a SIMD issues the
+// first in 8 cycles, the others in 2, so vector issue is the bound (memory moves 8 bytes per token and channel in 16-bit storage).
+//
+// Long sequences are cut into tiles that are walked side by side:
+//   k_packed_ends    every tile but a sequence's last, from a zero state: its end state E and the sum of its step sizes
+//   k_packed_chain   per sequence, over its tiles: h_k+1 = exp(A sum) h_k + E_k; leaves in E's place the state the tile begins with
+//   k_packed_scan    every tile from that state; the last one leaves the sequence's state in its slot
+// Sequences of one tile need the last kernel alone: its wave reads the slot before it writes it.  In longer ones k_packed_chain has
+// read the slot before any tile writes it.
+#include <hip/hip_runtime.h>
+
+#include "corey_packed_scan.h"
+
+namespace {
+
+using namespace corey_packed;
+
+template <typename T, bool NEIGHBOURS, int GROUPS>
+__global__ __launch_bounds__(64 * GROUPS, 2) void k_packed_ends(PackedScanArgs a)
+{
+    __shared__ __align__(16) float s_b[GROUPS][2][kStates * K];
+    const int wave = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, lane = (int)threadIdx.x & 63;
+    const int n0 = wave * kStates;
+    const int tile = (int)(blockIdx.x / (unsigned)a.groups);
+    const Piece p = a.ix.tiles[tile];
+    if (!a.ix.good() || p.seq < 0 || (p.bits & 2) || n0 >= a.N) return;
+    const Channels<NEIGHBOURS> c((int)(blockIdx.x % (unsigned)a.groups), lane, a.D);
+    States s;
+    load_a(s, a.A, c.d, n0, a.N);
+    float bias[2], sum[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) bias[i] = a.bias ? a.bias[c.d[i]] : 0.f;
+#pragma unroll
+    for (int n = 0; n < kStates; ++n) s.h[n][0] = s.h[n][1] = 0.f;
+    Block<T> now;
+    request<T, false, false, false>(now, a, c, n0, p.first, p.count);
+    int buf = 0;
+    for (int t0 = 0; t0 < p.count; t0 += K, buf ^= 1) {
+        float dl[2 * K], dx[2 * K], u[2 * K];
+        float* sb = s_b[wave][buf];
+        stage<T, false>(now, sb, nullptr);
+        steps<T>(now, bias, a.softplus != 0, p.count - t0, dl, dx, u);
+        if (t0 + K < p.count) request<T, false, false, false>(now, a, c, n0, p.first + t0 + K, p.count - t0 - K);
+#pragma unroll
+        for (int t = 0; t < K; ++t) {
+            sum[0] += dl[2 * t];
+            sum[1] += dl[2 * t + 1];
+        }
+        lds_in_order();
+        Words<K> bv[2];
+        bv[0] = words<K>(sb);
+#pragma unroll
+        for (int n = 0; n < kStates; ++n) {
+            if (n + 1 < kStates) bv[(n + 1) & 1] = words<K>(sb + (n + 1) * K);
+            float d[2 * K];
+#pragma unroll
+            for (int i = 0; i < 2 * K; ++i) d[i] = dl[i] * s.a2[n][i & 1];
+            exp2_burst<2 * K>(d);
+#pragma unroll
+            for (int t = 0; t < K; ++t) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s.h[n][i] = fmaf(d[2 * t + i], s.h[n][i], dx[2 * t + i] * bv[n & 1].v[t]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    float* out = a.ends + ((int64_t)tile * a.N + n0) * a.D;
+#pragma unroll
+    for (int n = 0; n < kStates; ++n) {
+        if (n0 + n < a.N) {
+            if (c.on[0]) out[(int64_t)n * a.D + c.d[0]] = s.h[n][0];
+            if (c.on[1]) out[(int64_t)n * a.D + c.d[1]] = s.h[n][1];
+        }
+    }
+    if (wave == 0) {
+        if (c.on[0]) a.sums[(int64_t)tile * a.D + c.d[0]] = sum[0];
+        if (c.on[1]) a.sums[(int64_t)tile * a.D + c.d[1]] = sum[1];
+    }
+}
+
+// A lane is one channel and state of one sequence.  The tiles' values are requested kAhead at a time.
+constexpr int kAhead = 8;
+__global__ __launch_bounds__(256) void k_packed_chain(PackedScanArgs a, int columns)
+{
+    const int which = (int)(blockIdx.x / (unsigned)columns);
+    const int64_t col = (int64_t)(blockIdx.x % (unsigned)columns) * 256 + threadIdx.x;
+    if (!a.ix.good() || which >= a.ix.head[7] || col >= (int64_t)a.D * a.N) return;
+    const int seq = a.ix.longs[which];
+    const int first = a.ix.tile_begin[seq], stop = a.ix.tile_begin[seq + 1];
+    const int n = (int)(col / a.D), d = (int)(col % a.D);
+    const float a2 = a.A[(int64_t)d * a.N + n] * kLog2e;
+    const int64_t slot = slot_of(a.slots, seq, a.n_slots), wide = (int64_t)a.N * a.D;
+    float h = slot >= 0 ? a.state[(slot * a.D + d) * a.N + n] : 0.f;
+    float* e = a.ends + col;
+    const float* sums = a.sums + d;
+    for (int k0 = first; k0 < stop; k0 += kAhead) {
+        float end[kAhead], sum[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t k = min(k0 + i, stop - 2);             // (the last tile has no end state)
+            end[i] = e[k * wide];
+            sum[i] = sums[k * a.D];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (k0 + i < stop) {
+                e[(k0 + i) * wide] = h;
+                h = fmaf(fast_exp2(a2 * sum[i]), h, end[i]);
+            }
+        }
+    }
+}
+
+template <typename T, bool NEIGHBOURS, bool GATED, int GROUPS>
+__global__ __launch_bounds__(64 * GROUPS, 2) void k_packed_scan(PackedScanArgs a)
+{
+    __shared__ __align__(16) float s_b[GROUPS][2][kStates * K], s_c[GROUPS][2][kStates * K];
+    __shared__ float s_part[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? 2 * K * 64 : 1];
+    const int wave = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, lane = (int)threadIdx.x & 63;
+    const int n0 = wave * kStates;
+    const int tile = (int)(blockIdx.x / (unsigned)a.groups);
+    const Piece p = a.ix.tiles[tile];
+    if (!a.ix.good() || p.seq < 0) return;                       // (the same for every wave of the workgroup)
+    const Channels<NEIGHBOURS> c((int)(blockIdx.x % (unsigned)a.groups), lane, a.D);
+    States s;
+    load_a(s, a.A, c.d, n0, a.N);
+    float bias[2], skip[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        bias[i] = a.bias ? a.bias[c.d[i]] : 0.f;
+        skip[i] = a.Dv && wave == 0 ? a.Dv[c.d[i]] : 0.f;
+    }
+    Block<T> now;
+    request<T, true, GATED, false>(now, a, c, n0, p.first, p.count);
+    // the state the tile begins with
+    const int64_t from = slot_of(a.slots, p.seq, a.n_slots);
+    if (p.bits == 3) {
+#pragma unroll
+        for (int n = 0; n < kStates; ++n) s.h[n][0] = s.h[n][1] = 0.f;
+        if (from >= 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float row[kStates];
+                load_row(row, a.state + (from * a.D + c.d[i]) * a.N + n0, n0, a.N);
+#pragma unroll
+                for (int n = 0; n < kStates; ++n) s.h[n][i] = row[n];
+            }
+        }
+    } else {
+        const float* start = a.ends + ((int64_t)tile * a.N + n0) * a.D;
+#pragma unroll
+        for (int n = 0; n < kStates; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s.h[n][i] = n0 + n < a.N ? start[(int64_t)n * a.D + c.d[i]] : 0.f;
+    }
+    int buf = 0;
+    for (int t0 = 0; t0 < p.count; t0 += K, buf ^= 1) {
+        const int count = p.count - t0;
+        float dl[2 * K], dx[2 * K], acc[2 * K];
+        Two<T> gate[K];
+        float* sb = s_b[wave][buf];
+        float* sc = s_c[wave][buf];
+        stage<T, true>(now, sb, sc);
+        steps<T>(now, bias, a.softplus != 0, count, dl, dx, acc);
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) acc[i] *= skip[i & 1];   // the skip term D u opens the sum over the states
+        if constexpr (GATED) {
+#pragma unroll
+            for (int t = 0; t < K; ++t) gate[t] = now.z[t];
+        }
+        if (t0 + K < p.count) request<T, true, GATED, false>(now, a, c, n0, p.first + t0 + K, p.count - t0 - K);
+        lds_in_order();
+        Words<K> bv[2], cv[2];
+        bv[0] = words<K>(sb);
+        cv[0] = words<K>(sc);
+#pragma unroll
+        for (int n = 0; n < kStates; ++n) {
+            if (n + 1 < kStates) {
+                bv[(n + 1) & 1] = words<K>(sb + (n + 1) * K);
+                cv[(n + 1) & 1] = words<K>(sc + (n + 1) * K);
+            }
+            float d[2 * K];
+#pragma unroll
+            for (int i = 0; i < 2 * K; ++i) d[i] = dl[i] * s.a2[n][i & 1];
+            exp2_burst<2 * K>(d);
+#pragma unroll
+            for (int t = 0; t < K; ++t) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    s.h[n][i] = fmaf(d[2 * t + i], s.h[n][i], dx[2 * t + i] * bv[n & 1].v[t]);
+                    acc[2 * t + i] = fmaf(cv[n & 1].v[t], s.h[n][i], acc[2 * t + i]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (GROUPS > 1) {                              // the sum over the waves' states; wave 0 finishes
+            __syncthreads();
+            if (wave != 0) {
+#pragma unroll
+                for (int i = 0; i < 2 * K; ++i) s_part[wave][i * 64 + lane] = acc[i];
+            }
+            __syncthreads();
+            if (wave != 0) continue;
+            for (int w = 1; w < GROUPS; ++w) {
+#pragma unroll
+                for (int i = 0; i < 2 * K; ++i) acc[i] += s_part[w][i * 64 + lane];
+            }
+        }
+        if constexpr (GATED) {
+#pragma unroll
+            for (int i = 0; i < 2 * K; ++i) acc[i] *= silu(Io<T>::ld(&gate[i / 2].v[i & 1]));
+        }
+        // (the sums are done here: left to itself the compiler moves a token's sum over the states into the branch that stores it, and
+        // keeps the states of all tokens until then, in scratch memory)
+#pragma unroll
+        for (int i = 0; i < 2 * K; ++i) asm volatile("" : "+v"(acc[i]));
+        T* y = static_cast<T*>(a.y) + (int64_t)(p.first + t0) * a.y_stride;
+#pragma unroll
+        for (int t = 0; t < K; ++t)
+            if (t < count) store_two<T, NEIGHBOURS>(y + t * a.y_stride, c, acc[2 * t], acc[2 * t + 1]);
+    }
+    if (!(p.bits & 2)) return;
+    const int64_t to = slot_of(a.slots_out, p.seq, a.n_slots);
+    if (to < 0) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (!c.on[i]) continue;
+        float* out = a.state + (to * a.D + c.d[i]) * a.N + n0;
+        if (a.N % 4 == 0) {
+#pragma unroll
+            for (int n = 0; n < kStates; n += 4) {
+                const float q[4] = {s.h[n][i], s.h[n + 1][i], s.h[n + 2][i], s.h[n + 3][i]};
+                if (n0 + n < a.N) __builtin_memcpy(out + n, q, sizeof(q));
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < kStates; ++n)
+                if (n0 + n < a.N) out[n] = s.h[n][i];
+        }
+    }
+}
+
+// One token of every sequence.  As the state's update of a whole batch: a row of N states is spread over 2^k lanes of four states.
+struct StepArgs {
+    float* state;
+    const int32_t *slots, *slots_out;
+    const void *x, *delta, *Bt, *Ct, *z;
+    const float *A, *Dv, *bias;
+    void* y;
+    int64_t x_stride, d_stride, b_stride, c_stride, z_stride, y_stride, n_slots;
+    uint32_t rows, D;
+    int32_t N, lpr_log2, softplus;
+};
+
+template <typename T, bool VECTOR>
+__global__ __launch_bounds__(256) void k_packed_step(StepArgs a)
+{
+    const uint64_t gid = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const int LPR = 1 << a.lpr_log2, j = (int)(gid & (uint64_t)(LPR - 1)), n = 4 * j;
+    const uint32_t r = (uint32_t)(gid >> a.lpr_log2);
+    const bool active = r < a.rows;                              // whole rows are active or not: LPR divides the wave
+    const uint32_t row = active ? r : a.rows - 1;
+    const uint32_t b = row / a.D, d = row - b * a.D;
+    const int64_t from = slot_of(a.slots, (int)b, a.n_slots), to = slot_of(a.slots_out, (int)b, a.n_slots);
+    float h[4] = {}, av[4] = {}, bv[4] = {}, cv[4] = {};
+    const T* brow = static_cast<const T*>(a.Bt) + (int64_t)b * a.b_stride;
+    const T* crow = static_cast<const T*>(a.Ct) + (int64_t)b * a.c_stride;
+    if constexpr (VECTOR) {
+        if (n < a.N) {
+            T rb[4], rc[4];
+            __builtin_memcpy(av, a.A + (int64_t)d * a.N + n, sizeof(av));
+            __builtin_memcpy(rb, brow + n, sizeof(rb));
+            __builtin_memcpy(rc, crow + n, sizeof(rc));
+            if (from >= 0) {
+                const float4v q = *reinterpret_cast<const float4v*>(a.state + (from * a.D + d) * a.N + n);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = q[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bv[i] = Io<T>::ld(&rb[i]);
+                cv[i] = Io<T>::ld(&rc[i]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n + i < a.N) {
+                av[i] = a.A[(int64_t)d * a.N + n + i];
+                bv[i] = Io<T>::ld(brow + n + i);
+                cv[i] = Io<T>::ld(crow + n + i);
+                if (from >= 0) h[i] = a.state[(from * a.D + d) * a.N + n + i];
+            }
+        }
+    }
+    const float xv = Io<T>::ld(static_cast<const T*>(a.x) + (int64_t)b * a.x_stride + d);
+    float dl = Io<T>::ld(static_cast<const T*>(a.delta) + (int64_t)b * a.d_stride + d) + (a.bias ? a.bias[d] : 0.f);
+    const float zv = a.z ? Io<T>::ld(static_cast<const T*>(a.z) + (int64_t)b * a.z_stride + d) : 0.f;
+    const float skip = a.Dv ? a.Dv[d] : 0.f;
+    if (a.softplus) dl = softplus(dl);
+    const float dx = dl * xv;
+    float acc = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (n + i < a.N) {
+            h[i] = fmaf(fast_exp2(dl * (av[i] * kLog2e)), h[i], dx * bv[i]);
+            acc = fmaf(cv[i], h[i], acc);
+        }
+    }
+    if (active && to >= 0) {
+        float* out = a.state + (to * a.D + d) * a.N + n;
+        if constexpr (VECTOR) {
+            if (n < a.N) *reinterpret_cast<float4v*>(out) = float4v{h[0], h[1], h[2], h[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n + i < a.N) out[i] = h[i];
+        }
+    }
+    for (int m = LPR >> 1; m >= 1; m >>= 1) acc += __shfl_xor(acc, m);
+    if (active && j == 0) {
+        float yv = a.Dv ? fmaf(skip, xv, acc) : acc;
+        if (a.z) yv *= silu(zv);
+        Io<T>::st(static_cast<T*>(a.y) + (int64_t)b * a.y_stride + d, yv);
+    }
+}
+
+}  // namespace
+
+// Tiles are what runs side by side: about four waves a SIMD fill the GPU (4096 of 128 channels and 16 states).  Longer tiles than
+// that needs mean fewer begun states to form and to carry, and none at all for the sequences that fit into one.
+extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
+{
+    if (S < 1 || T < 1 || D < 1 || N < 1) return 0;
+    if (backward) return N > 64 ? 32 : 64;
+    const double waves = (double)((D + 127) / 128) * (double)((N + 15) / 16);
+    const double most = (double)T * waves / 4096.0;
+    int32_t tile = COREY_PACK_BLOCK;
+    while (tile < 1024 && 2 * tile <= most) tile *= 2;
+    return tile;
+}
+
+extern "C" size_t corey_scan_packed_workspace(const corey_pack* pack, int64_t D, int64_t N)
+{
+    Index ix;
+    if (D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE || index_of("corey_scan_packed_workspace", pack, &ix)) return 0;
+    const Layout l = layout(pack->S, pack->T, pack->tile);
+    if (pack->T <= pack->tile) return 16;                        // no sequence has a second tile
+    return (size_t)l.max_tiles * (size_t)((N + 1) * D) * 4;
+}
+
+extern "C" int corey_scan_packed(const void* u, int64_t u_stride, const void* delta, int64_t delta_stride, const float* A, const void* Bm,
+                                 int64_t B_stride, const void* Cm, int64_t C_stride, const float* Dv, const void* z, int64_t z_stride,
+                                 const float* delta_bias, int delta_softplus, float* state, int64_t n_slots, const int32_t* slots,
+                                 const int32_t* slots_out, const corey_pack* pack, void* y, int64_t y_stride, corey_dtype dt, int64_t D,
+                                 int64_t N, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    using corey::fail;
+    const char* who = "corey_scan_packed";
+    if (!u || !delta || !A || !Bm || !Cm || !y) return fail(COREY_ENULL, "%s: u, delta, A, Bm, Cm and y are required", who);
+    if (!good_dtype(dt)) return fail(COREY_EINVAL, "%s: unknown dtype %d", who, (int)dt);
+    if (D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1) return fail(COREY_ESHAPE, "%s: 1 <= D <= %d and N >= 1 required", who, COREY_PACK_MAX_CHANNELS);
+    if (N > COREY_PACK_MAX_STATE) return fail(COREY_EUNSUPPORTED, "%s: N above %d", who, COREY_PACK_MAX_STATE);
+    if (!good_stride(u_stride, D) || !good_stride(delta_stride, D) || !good_stride(y_stride, D) || (z && !good_stride(z_stride, D)) ||
+        !good_stride(B_stride, N) || !good_stride(C_stride, N))
+        return fail(COREY_ESHAPE, "%s: rows must be at least D (B and C: N) apart", who);
+    if ((slots || slots_out) && (!state || n_slots < 1)) return fail(COREY_ENULL, "%s: slots need a pool of states", who);
+    if (y == u || y == delta || y == Bm || y == Cm || y == z) return fail(COREY_EINVAL, "%s: y may not be an input", who);
+    PackedScanArgs a = {};
+    if (int e = index_of(who, pack, &a.ix)) return e;
+    if (!workspace || workspace_bytes < corey_scan_packed_workspace(pack, D, N) || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+        return fail(COREY_EWORKSPACE, "%s: workspace missing, misaligned or smaller than corey_scan_packed_workspace()", who);
+    const Layout l = layout(pack->S, pack->T, pack->tile);
+    a.u = u; a.delta = delta; a.Bm = Bm; a.Cm = Cm; a.z = z;
+    a.A = A; a.Dv = Dv; a.bias = delta_bias;
+    a.y = y;
+    a.state = state; a.slots = slots; a.slots_out = slots_out ? slots_out : slots; a.n_slots = n_slots;
+    a.u_stride = u_stride; a.d_stride = delta_stride; a.b_stride = B_stride; a.c_stride = C_stride; a.z_stride = z_stride; a.y_stride = y_stride;
+    a.ends = static_cast<float*>(workspace);
+    a.sums = a.ends + l.max_tiles * N * D;
+    a.D = (int32_t)D; a.N = (int32_t)N;
+    a.softplus = delta_softplus ? 1 : 0;
+    a.tiles = (int32_t)l.max_tiles;
+    a.groups = (int32_t)((D + 127) / 128);
+    const int64_t grid = l.max_tiles * a.groups, columns = (D * N + 255) / 256;
+    if (grid > INT32_MAX || columns * (l.max_longs + 1) > INT32_MAX) return fail(COREY_ESHAPE, "%s: T * D is too large", who);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    by_type(dt, [&](auto t) {
+        using T = decltype(t);
+        by_groups(N, [&](auto g) {
+            constexpr int G = decltype(g)::value;
+            auto go = [&](auto near) {
+                constexpr bool P = decltype(near)::value;
+                if (pack->T > pack->tile) {
+                    k_packed_ends<T, P, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
+                    k_packed_chain<<<(unsigned)(columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
+                }
+                if (z) k_packed_scan<T, P, true, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
+                else k_packed_scan<T, P, false, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
+            };
+            if (D % 2 == 0) go(std::true_type());
+            else go(std::false_type());
+        });
+    });
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? corey::hip_fail(e, "corey_scan_packed launch") : COREY_OK;
+}
+
+extern "C" int corey_scan_packed_step(float* state, int64_t n_slots, const int32_t* slots, const int32_t* slots_out, const void* x,
+                                      int64_t x_stride, const void* delta, int64_t delta_stride, const float* A, const void* Bt,
+                                      int64_t B_stride, const void* Ct, int64_t C_stride, const float* Dv, const void* z, int64_t z_stride,
+                                      const float* delta_bias, int delta_softplus, void* y, int64_t y_stride, corey_dtype dt, int64_t S,
+                                      int64_t D, int64_t N, void* hip_stream)
+{
+    using corey::fail;
+    const char* who = "corey_scan_packed_step";
+    if (!state || !slots || !x || !delta || !A || !Bt || !Ct || !y)
+        return fail(COREY_ENULL, "%s: state, slots, x, delta, A, Bt, Ct and y are required", who);
+    if (!good_dtype(dt)) return fail(COREY_EINVAL, "%s: unknown dtype %d", who, (int)dt);
+    if (S < 1 || D < 1 || N < 1 || n_slots < 1 || N > COREY_MAX_STATE)
+        return fail(COREY_ESHAPE, "%s: S, D, n_slots >= 1 and 1 <= N <= %d required", who, COREY_MAX_STATE);
+    if ((double)S * (double)D >= 33554432.0) return fail(COREY_ESHAPE, "%s: S*D must stay below 2^25", who);
+    if (!good_stride(x_stride, D) || !good_stride(delta_stride, D) || !good_stride(y_stride, D) || (z && !good_stride(z_stride, D)) ||
+        !good_stride(B_stride, N) || !good_stride(C_stride, N))
+        return fail(COREY_ESHAPE, "%s: rows must be at least D (Bt and Ct: N) apart", who);
+    if (reinterpret_cast<uintptr_t>(state) % 4 != 0) return fail(COREY_EINVAL, "%s: state must be 4-byte aligned", who);
+    if (y == x || y == delta || y == Bt || y == Ct || y == z) return fail(COREY_EINVAL, "%s: y may not be an input", who);
+    StepArgs a;
+    a.state = state; a.slots = slots; a.slots_out = slots_out ? slots_out : slots;
+    a.x = x; a.delta = delta; a.Bt = Bt; a.Ct = Ct; a.z = z;
+    a.A = A; a.Dv = Dv; a.bias = delta_bias;
+    a.y = y;
+    a.x_stride = x_stride; a.d_stride = delta_stride; a.b_stride = B_stride; a.c_stride = C_stride; a.z_stride = z_stride; a.y_stride = y_stride;
+    a.n_slots = n_slots;
+    a.rows = (uint32_t)(S * D);
+    a.D = (uint32_t)D;
+    a.N = (int32_t)N;
+    a.lpr_log2 = 0;
+    while ((1 << a.lpr_log2) < (N + 3) / 4) ++a.lpr_log2;
+    a.softplus = delta_softplus ? 1 : 0;
+    const unsigned blocks = (unsigned)((((uint64_t)(S * D) << a.lpr_log2) + 255) / 256);
+    const bool vector = N % 4 == 0 && reinterpret_cast<uintptr_t>(state) % 16 == 0;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    by_type(dt, [&](auto t) {
+        using T = decltype(t);
+        if (vector) k_packed_step<T, true><<<blocks, 256, 0, stream>>>(a);
+        else k_packed_step<T, false><<<blocks, 256, 0, stream>>>(a);
+    });
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? corey::hip_fail(e, "corey_scan_packed_step launch") : COREY_OK;
+}

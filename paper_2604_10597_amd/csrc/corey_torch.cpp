@@ -15,6 +15,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -41,6 +42,16 @@ struct Lib {
     COREY_FN(selective_scan_fwd_routed);
     COREY_FN(selective_scan_fwd_workspace);
     COREY_FN(selective_state_update);
+    COREY_FN(corey_pack_plan);
+    COREY_FN(corey_pack_bytes);
+    COREY_FN(corey_conv_packed);
+    COREY_FN(corey_conv_packed_bwd);
+    COREY_FN(corey_conv_packed_bwd_workspace);
+    COREY_FN(corey_scan_packed);
+    COREY_FN(corey_scan_packed_workspace);
+    COREY_FN(corey_scan_packed_step);
+    COREY_FN(corey_scan_packed_bwd);
+    COREY_FN(corey_scan_packed_bwd_workspace);
     COREY_FN(corey_last_error);
 #undef COREY_FN
 };
@@ -708,6 +719,320 @@ PyObject* scan(PyObject* const* a)
     return PyTuple_Pack(2, ry.o, rl.o);
 }
 
+// ------------------------------------------------------------------------------------------- packed batches
+// These calls take tensors of any one device, whether it is the current one or not, and use that device's current stream.
+struct Where {
+    at::Device device;
+    c10::DeviceGuard guard;
+    void* stream;
+    explicit Where(const at::Tensor& t) : device(t.device()), guard(t.device()), stream(c10::hip::getCurrentHIPStream(t.device().index()).stream()) {}
+    void same(const at::Tensor* t, const char* name) const
+    {
+        if (t && t->defined() && t->device() != device) raise(PyExc_ValueError, "%s is on another device", name);
+    }
+    void same(const at::Tensor& t, const char* name) const { same(&t, name); }
+};
+
+// Rows of values without gaps, a constant number of elements apart: [n, wide] of this type.
+struct Rows {
+    const at::Tensor* t = nullptr;
+    int64_t stride = 0;
+    void* ptr() const { return t ? t->data_ptr() : nullptr; }
+};
+Rows rows_of(const at::Tensor* t, const char* name, at::ScalarType type, int64_t n, int64_t wide)
+{
+    Rows r;
+    if (!t) return r;
+    if (!t->is_cuda()) raise(PyExc_ValueError, "%s must be a GPU tensor", name);
+    if (t->scalar_type() != type || t->dim() != 2 || t->size(0) != n || t->size(1) != wide) want(t, name, type, {n, wide});
+    if (wide > 1 && t->stride(1) != 1) raise(PyExc_ValueError, "%s must have its rows' values side by side", name);
+    r.t = t;
+    r.stride = n > 1 ? t->stride(0) : wide;
+    if (r.stride < wide) raise(PyExc_ValueError, "%s has rows that overlap", name);
+    return r;
+}
+
+// A tensor argument of any strides; NULL for None.
+const at::Tensor* any_tensor(PyObject* o, const char* name)
+{
+    if (o == Py_None) return nullptr;
+    if (!THPVariable_Check(o)) raise(PyExc_TypeError, "%s must be a tensor", name);
+    return &THPVariable_Unpack(o);
+}
+const at::Tensor& rows_tensor(PyObject* o, const char* name)
+{
+    const at::Tensor* t = any_tensor(o, name);
+    if (!t) raise(PyExc_TypeError, "%s must be a tensor", name);
+    if (!t->is_cuda() || t->dim() != 2) raise(PyExc_ValueError, "%s must be a GPU tensor of rows, [T, D]", name);
+    return *t;
+}
+
+// binding.Pack: the index and the tensor that holds it.
+struct PackArg {
+    const corey_pack* pack;
+    Owned table;
+    PackArg(PyObject* o, const Where& w) : pack(structure<corey_pack>(o, "pack")), table(PyObject_GetAttrString(o, "table"))
+    {
+        if (!table.o) throw PyError{};
+        const at::Tensor& t = tensor(table.o, "pack.table");
+        w.same(t, "pack");
+        if (t.data_ptr() != pack->table || t.nbytes() < pack->bytes) raise(PyExc_ValueError, "pack is not as corey_pack_plan left it");
+    }
+};
+
+// The pool of states and the slots that go with a call.
+struct Pool {
+    const at::Tensor *state, *slots, *slots_out;
+    int64_t n_slots = 0;
+    Pool(PyObject* st, PyObject* in, PyObject* out, const Where& w, at::ScalarType type, int64_t S, int64_t D, int64_t N)
+        : state(optional_tensor(st, "state")), slots(optional_tensor(in, "slots")), slots_out(optional_tensor(out, "slots_out"))
+    {
+        if ((slots || slots_out) && !state) raise(PyExc_ValueError, "slots need a state");
+        if (state) {
+            if (state->dim() != 3) raise(PyExc_ValueError, "state must be [slots, D, %s]", "N (the convolution: W - 1)");
+            n_slots = state->size(0);
+            want(state, "state", type, {n_slots, D, N});
+        }
+        want(slots, "slots", at::kInt, {S});
+        want(slots_out, "slots_out", at::kInt, {S});
+        w.same(state, "state");
+        w.same(slots, "slots");
+        w.same(slots_out, "slots_out");
+    }
+};
+
+// An output: the caller's rows (a new reference to them), or new ones.
+struct OutRows {
+    at::Tensor made;
+    Rows r;
+    PyObject* given;
+    OutRows(PyObject* o, const char* name, const Where& w, at::ScalarType type, int64_t n, int64_t wide, const at::Tensor& like) : given(o)
+    {
+        const at::Tensor* t = any_tensor(o, name);
+        if (!t) {
+            made = empty({n, wide}, type, like);
+            t = &made;
+        }
+        w.same(*t, name);
+        r = rows_of(t, name, type, n, wide);
+    }
+    PyObject* result() const { return given != Py_None ? (Py_INCREF(given), given) : wrap(made); }
+};
+
+at::Tensor workspace_or_new(PyObject* o, size_t bytes, const Where& w, const at::Tensor& like)
+{
+    const at::Tensor* t = optional_tensor(o, "workspace");
+    if (t) {
+        w.same(t, "workspace");
+        return *t;
+    }
+    return empty({(int64_t)bytes < 16 ? 16 : (int64_t)bytes}, at::kByte, like);
+}
+
+PyObject* pack_plan(PyObject* const* a)      // lengths, T, tile, table, pack
+{
+    const at::Tensor& lengths = tensor(a[0], "lengths");
+    if (lengths.scalar_type() != at::kInt || lengths.dim() != 1) raise(PyExc_TypeError, "lengths must be int32 [S]");
+    const int64_t S = lengths.size(0), T = integer(a[1]);
+    const int32_t tile = integer32(a[2]);
+    const Where w(lengths);
+    const size_t need = lib.corey_pack_bytes(S, T, tile);
+    const at::Tensor* given = optional_tensor(a[3], "table");
+    at::Tensor table;
+    if (given) {
+        if (given->scalar_type() != at::kInt || given->dim() != 1) raise(PyExc_TypeError, "table must be int32 [words]");
+        w.same(given, "table");
+        table = *given;
+    } else {
+        table = empty({(int64_t)(need / 4)}, at::kInt, lengths);      // (invalid arguments: empty, and the library says what is wrong)
+    }
+    corey_pack* pack = structure<corey_pack>(a[4], "pack");
+    static int32_t none;                                              // stands in for the memory of an empty tensor
+    call([&] {
+        return lib.corey_pack_plan(ptr_as<int32_t>(lengths), S, T, tile, table.numel() ? table.data_ptr() : &none, table.nbytes(), pack, w.stream);
+    });
+    return wrap(table);
+}
+
+PyObject* conv_packed(PyObject* const* a)      // x, weight, bias, pack, state, slots, slots_out, u
+{
+    const at::Tensor& xt = rows_tensor(a[0], "x");
+    const Where w(xt);
+    const at::Tensor& weight = tensor(a[1], "weight");
+    const at::Tensor* bias = optional_tensor(a[2], "bias");
+    const PackArg p(a[3], w);
+    const int64_t T = p.pack->T, S = p.pack->S, D = xt.size(1);
+    if (weight.dim() != 2) raise(PyExc_ValueError, "weight must be [D, W]");
+    const int64_t W = weight.size(1);
+    const at::ScalarType type = xt.scalar_type();
+    const corey_dtype dt = dtype_code(type);
+    want(&weight, "weight", at::kFloat, {D, W});
+    want(bias, "bias", at::kFloat, {D});
+    w.same(weight, "weight");
+    w.same(bias, "bias");
+    const Rows x = rows_of(&xt, "x", type, T, D);
+    const Pool pool(a[4], a[5], a[6], w, type, S, D, W - 1);
+    const OutRows u(a[7], "u", w, type, T, D, xt);
+    call([&] {
+        return lib.corey_conv_packed(x.ptr(), x.stride, ptr_as<float>(&weight), ptr_as<float>(bias), ptr(pool.state), pool.n_slots,
+                                     ptr_as<int32_t>(pool.slots), ptr_as<int32_t>(pool.slots_out), p.pack, u.r.ptr(), u.r.stride, dt, D,
+                                     (int32_t)W, w.stream);
+    });
+    return u.result();
+}
+
+PyObject* conv_packed_bwd(PyObject* const* a)      // x, weight, bias, du, pack, workspace
+{
+    const at::Tensor& xt = rows_tensor(a[0], "x");
+    const Where w(xt);
+    const at::Tensor& weight = tensor(a[1], "weight");
+    const at::Tensor* bias = optional_tensor(a[2], "bias");
+    const PackArg p(a[4], w);
+    const int64_t T = p.pack->T, D = xt.size(1);
+    if (weight.dim() != 2) raise(PyExc_ValueError, "weight must be [D, W]");
+    const int64_t W = weight.size(1);
+    const at::ScalarType type = xt.scalar_type();
+    const corey_dtype dt = dtype_code(type);
+    want(&weight, "weight", at::kFloat, {D, W});
+    want(bias, "bias", at::kFloat, {D});
+    const at::Tensor& dut = rows_tensor(a[3], "du");
+    w.same(weight, "weight");
+    w.same(bias, "bias");
+    w.same(dut, "du");
+    const Rows x = rows_of(&xt, "x", type, T, D), du = rows_of(&dut, "du", type, T, D);
+    const OutRows dx(Py_None, "dx", w, type, T, D, xt);
+    const at::Tensor dweight = empty({D, W}, at::kFloat, xt), dbias = empty({D}, at::kFloat, xt);
+    const at::Tensor ws = workspace_or_new(a[5], lib.corey_conv_packed_bwd_workspace(p.pack, D, (int32_t)W), w, xt);
+    call([&] {
+        return lib.corey_conv_packed_bwd(x.ptr(), x.stride, ptr_as<float>(&weight), ptr_as<float>(bias), du.ptr(), du.stride, p.pack,
+                                         dx.r.ptr(), dx.r.stride, ptr_as<float>(dweight), ptr_as<float>(dbias), dt, D, (int32_t)W, ptr(ws),
+                                         ws.nbytes(), w.stream);
+    });
+    const Owned rx(dx.result()), rw(wrap(dweight)), rb(wrap(dbias));
+    return PyTuple_Pack(3, rx.o, rw.o, rb.o);
+}
+
+// What the packed scans take alike: u, delta, A, Bm, Cm, then Dv, z, delta_bias at the places given.
+struct ScanRows {
+    const at::Tensor &ut, &At;
+    Where w;
+    int64_t n, D, N;
+    at::ScalarType type;
+    corey_dtype dt;
+    Rows u, delta, Bm, Cm, z;
+    const at::Tensor *Dv, *bias;
+    ScanRows(PyObject* pu, PyObject* pd, PyObject* pA, PyObject* pB, PyObject* pC, PyObject* pDv, PyObject* pz, PyObject* pbias, int64_t rows)
+        : ut(rows_tensor(pu, "u")), At(tensor(pA, "A")), w(ut), n(rows < 0 ? ut.size(0) : rows), D(ut.size(1)), type(ut.scalar_type()), dt(dtype_code(type)),
+          Dv(optional_tensor(pDv, "Dv")), bias(optional_tensor(pbias, "delta_bias"))
+    {
+        if (At.dim() != 2) raise(PyExc_ValueError, "A must be [D, N]");
+        N = At.size(1);
+        want(&At, "A", at::kFloat, {D, N});
+        const at::Tensor &dt_ = rows_tensor(pd, "delta"), &bt = rows_tensor(pB, "Bm"), &ct = rows_tensor(pC, "Cm");
+        const at::Tensor* zt = any_tensor(pz, "z");
+        u = rows_of(&ut, "u", type, n, D);
+        delta = rows_of(&dt_, "delta", type, n, D);
+        Bm = rows_of(&bt, "Bm", type, n, N);
+        Cm = rows_of(&ct, "Cm", type, n, N);
+        z = rows_of(zt, "z", type, n, D);
+        want(Dv, "Dv", at::kFloat, {D});
+        want(bias, "delta_bias", at::kFloat, {D});
+        w.same(At, "A");
+        w.same(dt_, "delta");
+        w.same(bt, "Bm");
+        w.same(ct, "Cm");
+        w.same(zt, "z");
+        w.same(Dv, "Dv");
+        w.same(bias, "delta_bias");
+    }
+};
+
+int64_t pack_rows(PyObject* o) { return structure<corey_pack>(o, "pack")->T; }
+
+PyObject* scan_packed(PyObject* const* a)      // u, delta, A, Bm, Cm, pack, Dv, z, delta_bias, delta_softplus, state, slots, slots_out, y, workspace
+{
+    const ScanRows r(a[0], a[1], a[2], a[3], a[4], a[6], a[7], a[8], pack_rows(a[5]));
+    const PackArg p(a[5], r.w);
+    const int softplus = truth(a[9]) ? 1 : 0;
+    const Pool pool(a[10], a[11], a[12], r.w, at::kFloat, p.pack->S, r.D, r.N);
+    const OutRows y(a[13], "y", r.w, r.type, r.n, r.D, r.ut);
+    const at::Tensor ws = workspace_or_new(a[14], lib.corey_scan_packed_workspace(p.pack, r.D, r.N), r.w, r.ut);
+    call([&] {
+        return lib.corey_scan_packed(r.u.ptr(), r.u.stride, r.delta.ptr(), r.delta.stride, ptr_as<float>(&r.At), r.Bm.ptr(), r.Bm.stride,
+                                     r.Cm.ptr(), r.Cm.stride, ptr_as<float>(r.Dv), r.z.ptr(), r.z.stride, ptr_as<float>(r.bias), softplus,
+                                     ptr_as<float>(pool.state), pool.n_slots, ptr_as<int32_t>(pool.slots), ptr_as<int32_t>(pool.slots_out),
+                                     p.pack, y.r.ptr(), y.r.stride, r.dt, r.D, r.N, ptr(ws), ws.nbytes(), r.w.stream);
+    });
+    return y.result();
+}
+
+PyObject* scan_packed_step(PyObject* const* a)      // state, slots, x, delta, A, Bt, Ct, Dv, z, delta_bias, delta_softplus, slots_out, y
+{
+    const ScanRows r(a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], -1);
+    const int softplus = truth(a[10]) ? 1 : 0;
+    const Pool pool(a[0], a[1], a[11], r.w, at::kFloat, r.n, r.D, r.N);
+    if (!pool.state || !pool.slots) raise(PyExc_TypeError, "%s must be tensors", "state and slots");
+    const OutRows y(a[12], "y", r.w, r.type, r.n, r.D, r.ut);
+    call([&] {
+        return lib.corey_scan_packed_step(ptr_as<float>(pool.state), pool.n_slots, ptr_as<int32_t>(pool.slots), ptr_as<int32_t>(pool.slots_out),
+                                          r.u.ptr(), r.u.stride, r.delta.ptr(), r.delta.stride, ptr_as<float>(&r.At), r.Bm.ptr(), r.Bm.stride,
+                                          r.Cm.ptr(), r.Cm.stride, ptr_as<float>(r.Dv), r.z.ptr(), r.z.stride, ptr_as<float>(r.bias), softplus,
+                                          y.r.ptr(), y.r.stride, r.dt, r.n, r.D, r.N, r.w.stream);
+    });
+    return y.result();
+}
+
+PyObject* scan_packed_bwd(PyObject* const* a)      // u, delta, A, Bm, Cm, pack, dy, Dv, z, delta_bias, delta_softplus, out, workspace
+{
+    const ScanRows r(a[0], a[1], a[2], a[3], a[4], a[7], a[8], a[9], pack_rows(a[5]));
+    const PackArg p(a[5], r.w);
+    const at::Tensor& dyt = rows_tensor(a[6], "dy");
+    r.w.same(dyt, "dy");
+    const Rows dy = rows_of(&dyt, "dy", r.type, r.n, r.D);
+    const int softplus = truth(a[10]) ? 1 : 0;
+    const Owned out(a[11] != Py_None ? (Py_INCREF(a[11]), a[11]) : PyDict_New());
+    if (!out.o) throw PyError{};
+    // a gradient: the dict's, or a new one of [n, wide] (of [wide] for n = 0)
+    auto entry_of = [&](const char* name, at::ScalarType type, int64_t n, int64_t wide) {
+        at::Tensor t = a[11] != Py_None ? out_tensor(out.o, name, true) : at::Tensor();
+        if (!t.defined()) return n ? empty({n, wide}, type, r.ut) : empty({wide}, type, r.ut);
+        r.w.same(t, name);
+        return t;
+    };
+    auto rows_entry = [&](const at::Tensor& t, const char* name, int64_t wide) { return rows_of(&t, name, r.type, r.n, wide); };
+    const bool gated = r.z.t != nullptr;
+    const at::Tensor du = entry_of("du", r.type, r.n, r.D), dd = entry_of("ddelta", r.type, r.n, r.D), dB = entry_of("dB", r.type, r.n, r.N),
+                     dC = entry_of("dC", r.type, r.n, r.N), dA = entry_of("dA", at::kFloat, r.D, r.N);
+    const at::Tensor dz = gated ? entry_of("dz", r.type, r.n, r.D) : at::Tensor();
+    const at::Tensor dD = r.Dv ? entry_of("dD", at::kFloat, 0, r.D) : at::Tensor();
+    const at::Tensor dbias = r.bias ? entry_of("ddelta_bias", at::kFloat, 0, r.D) : at::Tensor();
+    const Rows rdu = rows_entry(du, "du", r.D), rdd = rows_entry(dd, "ddelta", r.D), rdB = rows_entry(dB, "dB", r.N), rdC = rows_entry(dC, "dC", r.N);
+    const Rows rdz = gated ? rows_entry(dz, "dz", r.D) : Rows();
+    want(dA, "dA", at::kFloat, {r.D, r.N});
+    want(dD, "dD", at::kFloat, {r.D});
+    want(dbias, "ddelta_bias", at::kFloat, {r.D});
+    for (const at::Tensor* t : {&dA, &dD, &dbias})
+        if (t->defined()) want_reachable(*t, "out[dA, dD, ddelta_bias]");
+    const at::Tensor ws = workspace_or_new(a[12], lib.corey_scan_packed_bwd_workspace(p.pack, r.D, r.N), r.w, r.ut);
+    call([&] {
+        return lib.corey_scan_packed_bwd(r.u.ptr(), r.u.stride, r.delta.ptr(), r.delta.stride, ptr_as<float>(&r.At), r.Bm.ptr(), r.Bm.stride,
+                                         r.Cm.ptr(), r.Cm.stride, ptr_as<float>(r.Dv), r.z.ptr(), r.z.stride, ptr_as<float>(r.bias), softplus,
+                                         dy.ptr(), dy.stride, p.pack, rdu.ptr(), rdu.stride, rdd.ptr(), rdd.stride, ptr_as<float>(dA), rdB.ptr(),
+                                         rdB.stride, rdC.ptr(), rdC.stride, ptr_as<float>(dD), rdz.ptr(), rdz.stride, ptr_as<float>(dbias),
+                                         r.dt, r.D, r.N, ptr(ws), ws.nbytes(), r.w.stream);
+    });
+    put(out.o, "du", du);
+    put(out.o, "ddelta", dd);
+    put(out.o, "dA", dA);
+    put(out.o, "dB", dB);
+    put(out.o, "dC", dC);
+    if (gated) put(out.o, "dz", dz);
+    if (r.Dv) put(out.o, "dD", dD);
+    if (r.bias) put(out.o, "ddelta_bias", dbias);
+    Py_INCREF(out.o);
+    return out.o;
+}
+
 // attach(path of libcorey.so, CoreyError, DeferredRoute): take the library's functions.  The library is loaded already.
 PyObject* attach(PyObject*, PyObject* args)
 {
@@ -741,6 +1066,16 @@ PyObject* attach(PyObject*, PyObject* args)
     COREY_FN(selective_scan_fwd_routed)
     COREY_FN(selective_scan_fwd_workspace)
     COREY_FN(selective_state_update)
+    COREY_FN(corey_pack_plan)
+    COREY_FN(corey_pack_bytes)
+    COREY_FN(corey_conv_packed)
+    COREY_FN(corey_conv_packed_bwd)
+    COREY_FN(corey_conv_packed_bwd_workspace)
+    COREY_FN(corey_scan_packed)
+    COREY_FN(corey_scan_packed_workspace)
+    COREY_FN(corey_scan_packed_step)
+    COREY_FN(corey_scan_packed_bwd)
+    COREY_FN(corey_scan_packed_bwd_workspace)
     COREY_FN(corey_last_error)
 #undef COREY_FN
     lib = l;
@@ -768,6 +1103,12 @@ PyMethodDef methods[] = {
     COREY_ENTRY("corey_route_device_deferred", route<true>, 11),
     COREY_ENTRY("corey_select_chunk_device", select_chunk_device, 5),
     COREY_ENTRY("selective_scan_fwd", scan, 19),
+    COREY_ENTRY("corey_pack_plan", pack_plan, 5),
+    COREY_ENTRY("corey_conv_packed", conv_packed, 8),
+    COREY_ENTRY("corey_conv_packed_bwd", conv_packed_bwd, 6),
+    COREY_ENTRY("corey_scan_packed", scan_packed, 15),
+    COREY_ENTRY("corey_scan_packed_step", scan_packed_step, 13),
+    COREY_ENTRY("corey_scan_packed_bwd", scan_packed_bwd, 13),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "libcorey on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
