@@ -417,7 +417,7 @@ int selective_state_update(void* state, const void* x, const void* delta, const 
  * operators are those of causal_conv1d_silu_fwd, selective_scan_fwd and selective_state_update (Method, Preliminaries) for every
  * sequence by itself, and their gradients.
  *   - Activations (x, u, delta, z, y, ...) are token-major, as the projections around them write and read them: row t holds
- *     token t's D channels (or N states, B and C) without gaps, and rows lie `..._stride` elements apart (>= D, or N; < 2^31).
+ *     token t's D channels (or N states, B and C) without gaps, and rows lie `..._stride` elements apart (>= D, or N; < 2^25).
  *     Any alignment is taken.  An output may not overlap an input or another output (an output that IS an input is refused).
  *   - Rows behind the last sequence (T may be more than the lengths add up to) are neither read nor written.
  *   - slots, slots_out   DEVICE int32[S]: sequence s begins from pool entry slots[s] and leaves its state in slots_out[s].

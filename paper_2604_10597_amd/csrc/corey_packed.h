@@ -44,7 +44,8 @@ inline Layout layout(int64_t S, int64_t T, int32_t tile)
 struct Index {
     const int32_t* head;
     const int32_t* starts;
-    const int32_t* tile_begin;
+    const int32_t* tile_begin;            // [S + 1] the first tile of each sequence
+    const int32_t* block_begin;           // [S + 1] the first block
     const int32_t* longs;                 // the sequences of more than one tile, head[7] of them
     const Piece* tiles;
     const Piece* blocks;
@@ -69,6 +70,7 @@ inline int index_of(const char* who, const corey_pack* p, Index* ix)
     ix->head = w;
     ix->starts = w + l.starts;
     ix->tile_begin = w + l.tile_begin;
+    ix->block_begin = w + l.block_begin;
     ix->longs = w + l.longs;
     ix->tiles = reinterpret_cast<const Piece*>(w + l.tiles);
     ix->blocks = reinterpret_cast<const Piece*>(w + l.blocks);
@@ -86,8 +88,9 @@ __device__ __forceinline__ int64_t slot_of(const int32_t* slots, int seq, int64_
     return s >= 0 && s < n_slots ? s : -1;
 }
 
-// Rows of `stride` elements between tokens: at least D, and what a lane's offsets are formed from stays in 64 bits.
-inline bool good_stride(int64_t stride, int64_t D) { return stride >= D && stride < ((int64_t)1 << 31); }
+// Rows of `stride` elements between tokens: at least D, and 15 of them stay below 2^31 bytes of the widest type.
+constexpr int64_t kMaxStride = (int64_t)1 << 25;
+inline bool good_stride(int64_t stride, int64_t D) { return stride >= D && stride < kMaxStride; }
 
 inline bool good_dtype(corey_dtype dt) { return dt == COREY_F32 || dt == COREY_BF16 || dt == COREY_F16; }
 

@@ -2,10 +2,10 @@
 //
 //     dl = softplus(delta + bias);  h[n] <- exp(dl A[n]) h[n] + dl B[n] u;  y = (sum_n C[n] h[n] + D u) silu(z)
 //
-// Neighbouring channels lie side by side in memory, so a lane is a pair of channels and walks the tokens one after another: B and C
-// of a token are the same for the whole wave (one LDS word read by all lanes), the states stay in registers, and nothing is
-// exchanged between lanes.  Per token, channel and state that is one exponential and four plain instructions; a SIMD issues the
-// first in 8 cycles, the others in 2, so vector issue is the bound (memory moves 8 bytes per token and channel in 16-bit storage).
+// Channels lie side by side in memory, so a lane is a channel and walks the tokens one after another: B and C of a token are the same
+// for the whole wave and sit in scalar registers, the states stay in vector registers, and nothing is exchanged between lanes.  Per
+// token, channel and state that is one exponential and four plain instructions; a SIMD issues the first in 8 cycles, the others in 2,
+// so vector issue is the bound (memory moves 8 bytes per token and channel in 16-bit storage).
 //
 // Long sequences are cut into tiles that are walked side by side:
 //   k_packed_ends    every tile but a sequence's last, from a zero state: its end state E and the sum of its step sizes
@@ -20,68 +20,63 @@
 namespace {
 
 using namespace corey_packed;
+using corey_scan::float4v;
 
-template <typename T, bool NEIGHBOURS, int GROUPS>
-__global__ __launch_bounds__(64 * GROUPS, 2) void k_packed_ends(PackedScanArgs a)
+constexpr int K = kHalf;                  // tokens of a step of the loop: loaded, and their step sizes formed, together
+
+// WHOLE: every wave has 16 states (N = 16 GROUPS): no state's work stands behind a condition.
+template <typename T, int GROUPS, bool WHOLE>
+__global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_ends(PackedScanArgs a)
 {
-    __shared__ __align__(16) float s_b[GROUPS][2][kStates * K];
-    const int wave = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, lane = (int)threadIdx.x & 63;
-    const int n0 = wave * kStates;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups);
     const Piece p = a.ix.tiles[tile];
     if (!a.ix.good() || p.seq < 0 || (p.bits & 2) || n0 >= a.N) return;
-    const Channels<NEIGHBOURS> c((int)(blockIdx.x % (unsigned)a.groups), lane, a.D);
-    States s;
-    load_a(s, a.A, c.d, n0, a.N);
-    float bias[2], sum[2] = {};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) bias[i] = a.bias ? a.bias[c.d[i]] : 0.f;
-#pragma unroll
-    for (int n = 0; n < kStates; ++n) s.h[n][0] = s.h[n][1] = 0.f;
-    Block<T> now;
-    request<T, false, false, false>(now, a, c, n0, p.first, p.count);
-    int buf = 0;
-    for (int t0 = 0; t0 < p.count; t0 += K, buf ^= 1) {
-        float dl[2 * K], dx[2 * K], u[2 * K];
-        float* sb = s_b[wave][buf];
-        stage<T, false>(now, sb, nullptr);
-        steps<T>(now, bias, a.softplus != 0, p.count - t0, dl, dx, u);
-        if (t0 + K < p.count) request<T, false, false, false>(now, a, c, n0, p.first + t0 + K, p.count - t0 - K);
-#pragma unroll
-        for (int t = 0; t < K; ++t) {
-            sum[0] += dl[2 * t];
-            sum[1] += dl[2 * t + 1];
-        }
-        lds_in_order();
-        Words<K> bv[2];
-        bv[0] = words<K>(sb);
-#pragma unroll
-        for (int n = 0; n < kStates; ++n) {
-            if (n + 1 < kStates) bv[(n + 1) & 1] = words<K>(sb + (n + 1) * K);
-            float d[2 * K];
-#pragma unroll
-            for (int i = 0; i < 2 * K; ++i) d[i] = dl[i] * s.a2[n][i & 1];
-            exp2_burst<2 * K>(d);
-#pragma unroll
-            for (int t = 0; t < K; ++t) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) s.h[n][i] = fmaf(d[2 * t + i], s.h[n][i], dx[2 * t + i] * bv[n & 1].v[t]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    float* out = a.ends + ((int64_t)tile * a.N + n0) * a.D;
+    const int d = (int)(blockIdx.x % (unsigned)a.groups) * Shape<GROUPS>::channels + (GROUPS > 1 ? 0 : wave * 64) + lane;
+    if (d >= a.D) return;
+    const uint32_t off = (uint32_t)d * (uint32_t)sizeof(T);
+    Rows<T> u_rows(a.u, a.u_stride, p.first), d_rows(a.delta, a.d_stride, p.first);
+    Tokens<T, K> u = load_tokens<T, K>(u_rows, p.count, off), delta = load_tokens<T, K>(d_rows, p.count, off);
+    float h[kStates], a2[kStates], sum = 0.f;
+    load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
-        if (n0 + n < a.N) {
-            if (c.on[0]) out[(int64_t)n * a.D + c.d[0]] = s.h[n][0];
-            if (c.on[1]) out[(int64_t)n * a.D + c.d[1]] = s.h[n][1];
+        a2[n] *= kLog2e;
+        h[n] = 0.f;
+    }
+    const float bias = a.bias ? a.bias[d] : 0.f;
+    const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + n0) * 2 * kHalf;
+    for (int t0 = 0; t0 < p.count; t0 += K) {                    // (a tile that is not its sequence's last is whole)
+        State8 s[3];                                             // two states ahead
+        s[0] = state8(from);
+        s[1] = state8(from + 2 * kHalf);
+        float dl[K], dx[K];
+        steps<T, K>(u, delta, bias, a.softplus != 0, K, dl, dx);
+        const int left = p.count - t0 - K, on = left > 0 ? K : 0;  // (behind the last block: the same rows again, for nothing)
+        u_rows.advance(on);
+        d_rows.advance(on);
+        u = load_tokens<T, K>(u_rows, K, off);
+        delta = load_tokens<T, K>(d_rows, K, off);
+#pragma unroll
+        for (int t = 0; t < K; ++t) sum += dl[t];
+#pragma unroll
+        for (int n = 0; n < kStates; ++n) {
+            if (!WHOLE && n0 + n >= a.N) continue;
+            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);
+            float e[K], x[K];
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
+#pragma unroll
+            for (int t = 0; t < K; ++t) h[n] = fmaf(e[t], h[n], x[t]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        from += a.N * 2 * kHalf;
     }
-    if (wave == 0) {
-        if (c.on[0]) a.sums[(int64_t)tile * a.D + c.d[0]] = sum[0];
-        if (c.on[1]) a.sums[(int64_t)tile * a.D + c.d[1]] = sum[1];
-    }
+    float* out = a.ends + ((int64_t)tile * a.N + n0) * a.D + d;
+#pragma unroll
+    for (int n = 0; n < kStates; ++n)
+        if (n0 + n < a.N) out[(int64_t)n * a.D] = h[n];
+    if (n0 == 0) a.sums[(int64_t)tile * a.D + d] = sum;
 }
 
 // A lane is one channel and state of one sequence.  The tiles' values are requested kAhead at a time.
@@ -117,132 +112,113 @@ __global__ __launch_bounds__(256) void k_packed_chain(PackedScanArgs a, int colu
     }
 }
 
-template <typename T, bool NEIGHBOURS, bool GATED, int GROUPS>
-__global__ __launch_bounds__(64 * GROUPS, 2) void k_packed_scan(PackedScanArgs a)
+template <typename T, bool GATED, int GROUPS, bool WHOLE>
+__global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_scan(PackedScanArgs a)
 {
-    __shared__ __align__(16) float s_b[GROUPS][2][kStates * K], s_c[GROUPS][2][kStates * K];
-    __shared__ float s_part[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? 2 * K * 64 : 1];
-    const int wave = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, lane = (int)threadIdx.x & 63;
-    const int n0 = wave * kStates;
+    __shared__ float s_part[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? K * 64 : 1];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups);
     const Piece p = a.ix.tiles[tile];
     if (!a.ix.good() || p.seq < 0) return;                       // (the same for every wave of the workgroup)
-    const Channels<NEIGHBOURS> c((int)(blockIdx.x % (unsigned)a.groups), lane, a.D);
-    States s;
-    load_a(s, a.A, c.d, n0, a.N);
-    float bias[2], skip[2];
+    const int d = (int)(blockIdx.x % (unsigned)a.groups) * Shape<GROUPS>::channels + (GROUPS > 1 ? 0 : wave * 64) + lane;
+    if (d >= a.D) return;
+    const bool states = n0 < a.N;                                // (a workgroup's last waves may have no states)
+    const uint32_t off = (uint32_t)d * (uint32_t)sizeof(T);
+    Rows<T> u_rows(a.u, a.u_stride, p.first), d_rows(a.delta, a.d_stride, p.first), z_rows(GATED ? a.z : a.u, GATED ? a.z_stride : 0, p.first),
+        y_rows(a.y, a.y_stride, p.first);
+    Tokens<T, K> u = load_tokens<T, K>(u_rows, p.count, off), delta = load_tokens<T, K>(d_rows, p.count, off);
+    float h[kStates], a2[kStates];
+    load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        bias[i] = a.bias ? a.bias[c.d[i]] : 0.f;
-        skip[i] = a.Dv && wave == 0 ? a.Dv[c.d[i]] : 0.f;
-    }
-    Block<T> now;
-    request<T, true, GATED, false>(now, a, c, n0, p.first, p.count);
+    for (int n = 0; n < kStates; ++n) a2[n] *= kLog2e;
+    const float bias = a.bias ? a.bias[d] : 0.f, skip = a.Dv && n0 == 0 ? a.Dv[d] : 0.f;
     // the state the tile begins with
-    const int64_t from = slot_of(a.slots, p.seq, a.n_slots);
     if (p.bits == 3) {
+        const int64_t slot = slot_of(a.slots, p.seq, a.n_slots);
+        if (slot >= 0) load_row<kStates>(h, a.state + (slot * a.D + d) * a.N + n0, n0, a.N);
+        else {
 #pragma unroll
-        for (int n = 0; n < kStates; ++n) s.h[n][0] = s.h[n][1] = 0.f;
-        if (from >= 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float row[kStates];
-                load_row(row, a.state + (from * a.D + c.d[i]) * a.N + n0, n0, a.N);
-#pragma unroll
-                for (int n = 0; n < kStates; ++n) s.h[n][i] = row[n];
-            }
+            for (int n = 0; n < kStates; ++n) h[n] = 0.f;
         }
     } else {
-        const float* start = a.ends + ((int64_t)tile * a.N + n0) * a.D;
+        const float* start = a.ends + ((int64_t)tile * a.N + n0) * a.D + d;
 #pragma unroll
-        for (int n = 0; n < kStates; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s.h[n][i] = n0 + n < a.N ? start[(int64_t)n * a.D + c.d[i]] : 0.f;
+        for (int n = 0; n < kStates; ++n) h[n] = n0 + n < a.N ? start[(int64_t)n * a.D] : 0.f;
     }
-    int buf = 0;
-    for (int t0 = 0; t0 < p.count; t0 += K, buf ^= 1) {
+    const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + (states ? n0 : 0)) * 2 * kHalf;
+    for (int t0 = 0; t0 < p.count; t0 += K) {
         const int count = p.count - t0;
-        float dl[2 * K], dx[2 * K], acc[2 * K];
-        Two<T> gate[K];
-        float* sb = s_b[wave][buf];
-        float* sc = s_c[wave][buf];
-        stage<T, true>(now, sb, sc);
-        steps<T>(now, bias, a.softplus != 0, count, dl, dx, acc);
-#pragma unroll
-        for (int i = 0; i < 2 * K; ++i) acc[i] *= skip[i & 1];   // the skip term D u opens the sum over the states
+        State8 s[3];                                             // two states ahead
+        s[0] = state8(from);
+        s[1] = state8(from + 2 * kHalf);
+        float dl[K], dx[K], acc[K];
+        Tokens<T, K> z;                                          // (needed at the end: requested now, not with the block before)
         if constexpr (GATED) {
-#pragma unroll
-            for (int t = 0; t < K; ++t) gate[t] = now.z[t];
+            z = load_tokens<T, K>(z_rows, count, off);
+            z_rows.advance(K);
         }
-        if (t0 + K < p.count) request<T, true, GATED, false>(now, a, c, n0, p.first + t0 + K, p.count - t0 - K);
-        lds_in_order();
-        Words<K> bv[2], cv[2];
-        bv[0] = words<K>(sb);
-        cv[0] = words<K>(sc);
+        steps<T, K>(u, delta, bias, a.softplus != 0, count, dl, dx);
+#pragma unroll
+        for (int t = 0; t < K; ++t) acc[t] = skip * u.at(t);     // the skip term D u opens the sum over the states
+        const bool more = count > K;                             // (behind the last block: the same rows again, for nothing)
+        u_rows.advance(more ? K : 0);
+        d_rows.advance(more ? K : 0);
+        u = load_tokens<T, K>(u_rows, more ? count - K : count, off);
+        delta = load_tokens<T, K>(d_rows, more ? count - K : count, off);
 #pragma unroll
         for (int n = 0; n < kStates; ++n) {
-            if (n + 1 < kStates) {
-                bv[(n + 1) & 1] = words<K>(sb + (n + 1) * K);
-                cv[(n + 1) & 1] = words<K>(sc + (n + 1) * K);
-            }
-            float d[2 * K];
-#pragma unroll
-            for (int i = 0; i < 2 * K; ++i) d[i] = dl[i] * s.a2[n][i & 1];
-            exp2_burst<2 * K>(d);
+            if (!WHOLE && n0 + n >= a.N) continue;
+            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);   // (behind the last: the next block's, or the end's)
+            float e[K], x[K];
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
 #pragma unroll
             for (int t = 0; t < K; ++t) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    s.h[n][i] = fmaf(d[2 * t + i], s.h[n][i], dx[2 * t + i] * bv[n & 1].v[t]);
-                    acc[2 * t + i] = fmaf(cv[n & 1].v[t], s.h[n][i], acc[2 * t + i]);
-                }
+                h[n] = fmaf(e[t], h[n], x[t]);
+                acc[t] = fmaf(s[n % 3].c(t), h[n], acc[t]);
+                // a state's share of the sums is added here: left to itself the compiler moves a token's sum over the states into the
+                // branch that stores it, and keeps the states of all tokens until then
+                asm volatile("" : "+v"(acc[t]), "+v"(h[n]));
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        from += a.N * 2 * kHalf;
         if constexpr (GROUPS > 1) {                              // the sum over the waves' states; wave 0 finishes
             __syncthreads();
             if (wave != 0) {
 #pragma unroll
-                for (int i = 0; i < 2 * K; ++i) s_part[wave][i * 64 + lane] = acc[i];
+                for (int t = 0; t < K; ++t) s_part[wave - 1][t * 64 + lane] = acc[t];
             }
             __syncthreads();
             if (wave != 0) continue;
-            for (int w = 1; w < GROUPS; ++w) {
+            for (int w = 0; w + 1 < GROUPS; ++w) {
 #pragma unroll
-                for (int i = 0; i < 2 * K; ++i) acc[i] += s_part[w][i * 64 + lane];
+                for (int t = 0; t < K; ++t) acc[t] += s_part[w][t * 64 + lane];
             }
         }
         if constexpr (GATED) {
+            float g[K];
+            gates<T, K>(z, g);
 #pragma unroll
-            for (int i = 0; i < 2 * K; ++i) acc[i] *= silu(Io<T>::ld(&gate[i / 2].v[i & 1]));
+            for (int t = 0; t < K; ++t) acc[t] *= g[t];
         }
-        // (the sums are done here: left to itself the compiler moves a token's sum over the states into the branch that stores it, and
-        // keeps the states of all tokens until then, in scratch memory)
-#pragma unroll
-        for (int i = 0; i < 2 * K; ++i) asm volatile("" : "+v"(acc[i]));
-        T* y = static_cast<T*>(a.y) + (int64_t)(p.first + t0) * a.y_stride;
-#pragma unroll
-        for (int t = 0; t < K; ++t)
-            if (t < count) store_two<T, NEIGHBOURS>(y + t * a.y_stride, c, acc[2 * t], acc[2 * t + 1]);
+        store_tokens<T, K>(y_rows, count, off, acc);
+        y_rows.advance(K);
     }
     if (!(p.bits & 2)) return;
     const int64_t to = slot_of(a.slots_out, p.seq, a.n_slots);
     if (to < 0) return;
+    float* out = a.state + (to * a.D + d) * a.N + n0;
+    if (a.N % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (!c.on[i]) continue;
-        float* out = a.state + (to * a.D + c.d[i]) * a.N + n0;
-        if (a.N % 4 == 0) {
-#pragma unroll
-            for (int n = 0; n < kStates; n += 4) {
-                const float q[4] = {s.h[n][i], s.h[n + 1][i], s.h[n + 2][i], s.h[n + 3][i]};
-                if (n0 + n < a.N) __builtin_memcpy(out + n, q, sizeof(q));
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < kStates; ++n)
-                if (n0 + n < a.N) out[n] = s.h[n][i];
+        for (int n = 0; n < kStates; n += 4) {
+            const float q[4] = {h[n], h[n + 1], h[n + 2], h[n + 3]};
+            if (n0 + n < a.N) __builtin_memcpy(out + n, q, sizeof(q));
         }
+    } else {
+#pragma unroll
+        for (int n = 0; n < kStates; ++n)
+            if (n0 + n < a.N) out[n] = h[n];
     }
 }
 
@@ -333,26 +309,41 @@ __global__ __launch_bounds__(256) void k_packed_step(StepArgs a)
 
 }  // namespace
 
-// Tiles are what runs side by side: about four waves a SIMD fill the GPU (4096 of 128 channels and 16 states).  Longer tiles than
+// Tiles are what runs side by side: about four waves a SIMD fill the GPU (4096 of 64 channels and 16 states).  Longer tiles than
 // that needs mean fewer begun states to form and to carry, and none at all for the sequences that fit into one.
 extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
 {
     if (S < 1 || T < 1 || D < 1 || N < 1) return 0;
-    if (backward) return N > 64 ? 32 : 64;
-    const double waves = (double)((D + 127) / 128) * (double)((N + 15) / 16);
+    const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16);
     const double most = (double)T * waves / 4096.0;
+    const int32_t longest = !backward ? 1024 : N > 64 ? 32 : 64;
     int32_t tile = COREY_PACK_BLOCK;
-    while (tile < 1024 && 2 * tile <= most) tile *= 2;
+    while (tile < longest && 2 * tile <= most) tile *= 2;
     return tile;
 }
+
+namespace {
+// The workspace's parts, in floats.
+struct Space {
+    int64_t bc, ends, sums, all;
+};
+Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
+{
+    const int64_t tiles = T > tile ? l.max_tiles : 0;            // (carried only where a sequence can have a second tile)
+    Space s;
+    s.bc = 0;
+    s.ends = s.bc + l.max_blocks * N * 32 + 32;                  // (the loop over the states asks for two more than there are)
+    s.sums = s.ends + tiles * N * D;
+    s.all = s.sums + tiles * D;
+    return s;
+}
+}  // namespace
 
 extern "C" size_t corey_scan_packed_workspace(const corey_pack* pack, int64_t D, int64_t N)
 {
     Index ix;
     if (D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE || index_of("corey_scan_packed_workspace", pack, &ix)) return 0;
-    const Layout l = layout(pack->S, pack->T, pack->tile);
-    if (pack->T <= pack->tile) return 16;                        // no sequence has a second tile
-    return (size_t)l.max_tiles * (size_t)((N + 1) * D) * 4;
+    return (size_t)space(layout(pack->S, pack->T, pack->tile), pack->T, pack->tile, D, N).all * 4;
 }
 
 extern "C" int corey_scan_packed(const void* u, int64_t u_stride, const void* delta, int64_t delta_stride, const float* A, const void* Bm,
@@ -382,29 +373,32 @@ extern "C" int corey_scan_packed(const void* u, int64_t u_stride, const void* de
     a.y = y;
     a.state = state; a.slots = slots; a.slots_out = slots_out ? slots_out : slots; a.n_slots = n_slots;
     a.u_stride = u_stride; a.d_stride = delta_stride; a.b_stride = B_stride; a.c_stride = C_stride; a.z_stride = z_stride; a.y_stride = y_stride;
-    a.ends = static_cast<float*>(workspace);
-    a.sums = a.ends + l.max_tiles * N * D;
+    const Space w = space(l, pack->T, pack->tile, D, N);
+    a.bc = static_cast<float*>(workspace) + w.bc;
+    a.ends = static_cast<float*>(workspace) + w.ends;
+    a.sums = static_cast<float*>(workspace) + w.sums;
     a.D = (int32_t)D; a.N = (int32_t)N;
     a.softplus = delta_softplus ? 1 : 0;
-    a.tiles = (int32_t)l.max_tiles;
-    a.groups = (int32_t)((D + 127) / 128);
-    const int64_t grid = l.max_tiles * a.groups, columns = (D * N + 255) / 256;
-    if (grid > INT32_MAX || columns * (l.max_longs + 1) > INT32_MAX) return fail(COREY_ESHAPE, "%s: T * D is too large", who);
+    a.blocks = (int32_t)l.max_blocks;
+    a.groups = (int32_t)channel_groups(D, N);
+    const int64_t grid = l.max_tiles * a.groups, columns = (D * N + 255) / 256, relay = (l.max_blocks * N * 32 + 255) / 256;
+    if (grid > INT32_MAX || relay > INT32_MAX || columns * (l.max_longs + 1) > INT32_MAX) return fail(COREY_ESHAPE, "%s: T * D is too large", who);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dt, [&](auto t) {
         using T = decltype(t);
+        k_packed_relay<T><<<(unsigned)relay, 256, 0, stream>>>(a);
         by_groups(N, [&](auto g) {
             constexpr int G = decltype(g)::value;
-            auto go = [&](auto near) {
-                constexpr bool P = decltype(near)::value;
+            const auto go = [&](auto whole) {
+                constexpr bool W = decltype(whole)::value;
                 if (pack->T > pack->tile) {
-                    k_packed_ends<T, P, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
+                    k_packed_ends<T, G, W><<<(unsigned)grid, 64 * Shape<G>::waves, 0, stream>>>(a);
                     k_packed_chain<<<(unsigned)(columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
                 }
-                if (z) k_packed_scan<T, P, true, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
-                else k_packed_scan<T, P, false, G><<<(unsigned)grid, 64 * G, 0, stream>>>(a);
+                if (z) k_packed_scan<T, true, G, W><<<(unsigned)grid, 64 * Shape<G>::waves, 0, stream>>>(a);
+                else k_packed_scan<T, false, G, W><<<(unsigned)grid, 64 * Shape<G>::waves, 0, stream>>>(a);
             };
-            if (D % 2 == 0) go(std::true_type());
+            if (N == G * kStates) go(std::true_type());
             else go(std::false_type());
         });
     });

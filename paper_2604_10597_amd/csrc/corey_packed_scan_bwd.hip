@@ -23,97 +23,89 @@ namespace {
 using namespace corey_packed;
 using corey_scan::dpp_move;
 
-constexpr int kTok = 16;                  // tokens of a block
+constexpr int kTok = kBlock;              // tokens of a block
 constexpr int kMaxBackTile = 64;
+constexpr int K = kHalf;                  // tokens of a step of k_packed_bwd_ends
 
-template <typename T, bool NEIGHBOURS, bool GATED, int GROUPS>
-__global__ __launch_bounds__(64 * GROUPS, 2) void k_packed_bwd_ends(PackedScanArgs a)
+template <typename T, bool GATED, int GROUPS, bool WHOLE>
+__global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_ends(PackedScanArgs a)
 {
-    __shared__ __align__(16) float s_b[GROUPS][2][kStates * K], s_c[GROUPS][2][kStates * K];
-    const int wave = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0, lane = (int)threadIdx.x & 63;
-    const int n0 = wave * kStates;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups);
     const Piece p = a.ix.tiles[tile];
     if (!a.ix.good() || p.seq < 0 || p.bits == 3 || n0 >= a.N) return;
-    const Channels<NEIGHBOURS> c((int)(blockIdx.x % (unsigned)a.groups), lane, a.D);
-    States s;
-    load_a(s, a.A, c.d, n0, a.N);
-    float bias[2], sum[2] = {}, back[kStates][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) bias[i] = a.bias ? a.bias[c.d[i]] : 0.f;
+    const int d = (int)(blockIdx.x % (unsigned)a.groups) * Shape<GROUPS>::channels + (GROUPS > 1 ? 0 : wave * 64) + lane;
+    if (d >= a.D) return;
+    const uint32_t off = (uint32_t)d * (uint32_t)sizeof(T);
+    Rows<T> u_rows(a.u, a.u_stride, p.first), d_rows(a.delta, a.d_stride, p.first), y_rows(a.dy, a.dy_stride, p.first),
+        z_rows(GATED ? a.z : a.u, GATED ? a.z_stride : 0, p.first);
+    Tokens<T, K> u, delta, dy, z;
+    const auto request = [&](int tokens, int count) {
+        u_rows.advance(tokens);
+        d_rows.advance(tokens);
+        y_rows.advance(tokens);
+        u = load_tokens<T, K>(u_rows, count, off);
+        delta = load_tokens<T, K>(d_rows, count, off);
+        dy = load_tokens<T, K>(y_rows, count, off);
+        if constexpr (GATED) {
+            z_rows.advance(tokens);
+            z = load_tokens<T, K>(z_rows, count, off);
+        }
+    };
+    request(0, p.count);
+    float h[kStates], a2[kStates], back[kStates], sum = 0.f;
+    load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) s.h[n][i] = back[n][i] = 0.f;
+        a2[n] *= kLog2e;
+        h[n] = back[n] = 0.f;
     }
-    Block<T> now;
-    request<T, true, GATED, true>(now, a, c, n0, p.first, p.count);
-    int buf = 0;
-    for (int t0 = 0; t0 < p.count; t0 += K, buf ^= 1) {
-        float dl[2 * K], dx[2 * K], ds[2 * K];
+    const float bias = a.bias ? a.bias[d] : 0.f;
+    const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + n0) * 2 * kHalf;
+    for (int t0 = 0; t0 < p.count; t0 += K) {
         const int count = p.count - t0;
-        float* sb = s_b[wave][buf];
-        float* sc = s_c[wave][buf];
-        stage<T, true>(now, sb, sc);
-        steps<T>(now, bias, a.softplus != 0, count, dl, dx, ds);
+        State8 s[3];                                             // two states ahead
+        s[0] = state8(from);
+        s[1] = state8(from + 2 * kHalf);
+        float dl[K], dx[K], ds[K];
+        steps<T, K>(u, delta, bias, a.softplus != 0, count, dl, dx);
+        if constexpr (GATED) gates<T, K>(z, ds);
 #pragma unroll
-        for (int i = 0; i < 2 * K; ++i) {
-            ds[i] = Io<T>::ld(&now.dy[i / 2].v[i & 1]);
-            if constexpr (GATED) ds[i] *= silu(Io<T>::ld(&now.z[i / 2].v[i & 1]));
-            ds[i] = i / 2 < count ? ds[i] : 0.f;
+        for (int t = 0; t < K; ++t) {
+            ds[t] = GATED ? ds[t] * dy.at(t) : dy.at(t);
+            if (count < K) ds[t] = t < count ? ds[t] : 0.f;
         }
-        const float before[2] = {sum[0], sum[1]};               // the decay up to this block is exp(A before)
+        const float before = sum;                                // the decay up to here is exp(A before)
 #pragma unroll
-        for (int i = 0; i < 2 * K; ++i) sum[i & 1] += dl[i];
-        if (t0 + K < p.count) request<T, true, GATED, true>(now, a, c, n0, p.first + t0 + K, count - K);
-        lds_in_order();
-        Words<K> bv[2], cv[2];
-        bv[0] = words<K>(sb);
-        cv[0] = words<K>(sc);
+        for (int t = 0; t < K; ++t) sum += dl[t];
+        request(count > K ? K : 0, count > K ? count - K : count);       // (behind the last block: the same rows again, for nothing)
 #pragma unroll
         for (int n = 0; n < kStates; ++n) {
-            if (n + 1 < kStates) {
-                bv[(n + 1) & 1] = words<K>(sb + (n + 1) * K);
-                cv[(n + 1) & 1] = words<K>(sc + (n + 1) * K);
-            }
-            float d[2 * K];
-#pragma unroll
-            for (int i = 0; i < 2 * K; ++i) d[i] = dl[i] * s.a2[n][i & 1];
-            exp2_burst<2 * K>(d);
+            if (!WHOLE && n0 + n >= a.N) continue;
+            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);   // (behind the last: the next block's, or the end's)
+            float e[K], x[K], g = 0.f;
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
 #pragma unroll
             for (int t = 0; t < K; ++t) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    s.h[n][i] = fmaf(d[2 * t + i], s.h[n][i], dx[2 * t + i] * bv[n & 1].v[t]);
-                }
+                h[n] = fmaf(e[t], h[n], x[t]);
+                const int r = K - 1 - t;                         // (and the gradients from the last token back)
+                g = fmaf(s[n % 3].c(r), ds[r], g) * e[r];
             }
-            float g[2] = {};
-#pragma unroll
-            for (int t = K - 1; t >= 0; --t) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) g[i] = fmaf(ds[2 * t + i], cv[n & 1].v[t], g[i]) * d[2 * t + i];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) back[n][i] = fmaf(fast_exp2(before[i] * s.a2[n][i]), g[i], back[n][i]);
+            back[n] = fmaf(fast_exp2(before * a2[n]), g, back[n]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        from += a.N * 2 * kHalf;
     }
-    const int64_t at = ((int64_t)tile * a.N + n0) * a.D;
+    const int64_t at = ((int64_t)tile * a.N + n0) * a.D + d;
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
         if (n0 + n < a.N) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (!c.on[i]) continue;
-                a.ends[at + (int64_t)n * a.D + c.d[i]] = s.h[n][i];
-                a.backs[at + (int64_t)n * a.D + c.d[i]] = back[n][i];
-            }
+            a.ends[at + (int64_t)n * a.D] = h[n];
+            a.backs[at + (int64_t)n * a.D] = back[n];
         }
     }
-    if (wave == 0) {
-        if (c.on[0]) a.sums[(int64_t)tile * a.D + c.d[0]] = sum[0];
-        if (c.on[1]) a.sums[(int64_t)tile * a.D + c.d[1]] = sum[1];
-    }
+    if (n0 == 0) a.sums[(int64_t)tile * a.D + d] = sum;
 }
 
 // A lane is one channel and state of one sequence, in one direction.  Leaves the state each tile begins with in `ends`, the gradient
@@ -179,203 +171,148 @@ __device__ __forceinline__ float fold16(float (&v)[16], int lane)
     return r;
 }
 
-// Waves of a workgroup: the channels' for up to 16 states (4 x 64 channels), the states' otherwise (64 channels).
-template <int GROUPS> constexpr int channel_waves() { return GROUPS == 1 ? 4 : 1; }
-template <int GROUPS> constexpr int back_waves() { return GROUPS * channel_waves<GROUPS>(); }
-__host__ __device__ constexpr int start_slots(int tile) { return tile > kTok ? tile / kTok - 1 : 1; }
-constexpr int kFold = 33;                 // floats of a state's folded sums in LDS: 16 tokens x (dB, dC), and one against bank conflicts
+// Values of a wave's states that it keeps in LDS, per lane: at the starts of blocks 1, 2, ... (a slot each), and the gradients.
+__host__ __device__ constexpr int kept(int tile) { return tile / kTok; }
 
+// The loop over the states is a loop (unrolled it is 50 KB of instructions, more than the instruction cache feeds), so what belongs to
+// a state from block to block stays out of registers: its value at the starts of the blocks and its gradient in LDS, its share of dA
+// in the workspace, where each lane adds to its own.
 template <typename T, bool GATED, int GROUPS>
-__global__ __launch_bounds__(64 * back_waves<GROUPS>(), 2) void k_packed_bwd(PackedScanArgs a)
+__global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(PackedScanArgs a)
 {
-    constexpr int CW = channel_waves<GROUPS>(), WAVES = back_waves<GROUPS>();
-    __shared__ __align__(16) float s_b[WAVES][kStates * kTok], s_c[WAVES][kStates * kTok];
-    __shared__ float s_fold[WAVES][kStates * kFold];
+    constexpr int WAVES = Shape<GROUPS>::waves;
+    __shared__ float s_fold[GROUPS == 1 ? WAVES : 1][GROUPS == 1 ? kStates * 2 * kTok : 1];
     __shared__ float s_part[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? 3 * kTok * 64 : 1];
-    extern __shared__ float s_starts[];   // [WAVES][slots][16 states][64 lanes]: states at the starts of blocks 1, 2, ...
+    extern __shared__ float s_kept[];     // [WAVES][kept(tile)][16 states][64 lanes]
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
     const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups), group = (int)(blockIdx.x % (unsigned)a.groups);
     const Piece p = a.ix.tiles[tile];
     if (!a.ix.good() || p.seq < 0) return;                       // (the same for every wave of the workgroup)
-    int d = (group * CW + (GROUPS > 1 ? 0 : wave)) * 64 + lane;
+    int d = group * Shape<GROUPS>::channels + (GROUPS > 1 ? 0 : wave * 64) + lane;
     const bool on = d < a.D;
     if (!on) d = a.D - 1;                                        // lanes without a channel: another's inputs, no gradient
-    float a2[kStates], g[kStates], dA[kStates];
-    load_row(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
+    const uint32_t off = (uint32_t)d * (uint32_t)sizeof(T);
+    const int mine = min(kStates, a.N - n0);                     // this wave's states; none in a workgroup's last waves perhaps
+    const int safe = mine > 0 ? n0 : 0;
     const float bias = a.bias ? a.bias[d] : 0.f, skip = a.Dv ? a.Dv[d] : 0.f;
-    const int64_t at = ((int64_t)tile * a.N + n0) * a.D + d;
     const bool sp = a.softplus != 0;
-    float dskip = 0.f, dbias = 0.f;
-#pragma unroll
-    for (int n = 0; n < kStates; ++n) {
-        a2[n] *= kLog2e;
-        dA[n] = 0.f;
-        g[n] = on && !(p.bits & 2) && n0 + n < a.N ? a.backs[at + (int64_t)n * a.D] : 0.f;
-    }
-    auto state_at_start = [&](int n) { return !(p.bits & 1) && n0 + n < a.N ? a.ends[at + (int64_t)n * a.D] : 0.f; };
-    float* starts = s_starts + (int64_t)wave * start_slots(a.ix.tile) * kStates * 64 + lane;
-    float* sb = s_b[wave];
-    float* sc = s_c[wave];
+    const int64_t block0 = first_block(a.ix, p);
+    const float* bc = a.bc + (block0 * 2 * a.N + safe) * 2 * kHalf;
+    const int half = a.N * 2 * kHalf;                            // from one half of a block to the next
+    const float* arow = a.A + (int64_t)d * a.N + safe;
+    const float* first_states = a.ends + ((int64_t)tile * a.N + safe) * a.D + d;
+    float* part = a.part_a + ((int64_t)tile * (a.N + 2) + safe) * a.D + d;
+    const bool begins = (p.bits & 1) != 0;                       // the sequence begins here, from zero
+    float* starts = s_kept + (int64_t)wave * kept(a.ix.tile) * kStates * 64 + lane;
+    float* grads = starts + (kept(a.ix.tile) - 1) * kStates * 64;
     const int blocks = (p.count + kTok - 1) / kTok;
-
-    // B (and C) of a block into this wave's LDS, [state][token]; a lane brings one token's states lane / 16 + 4 i
-    auto stage_bc = [&](int first, int count, auto with_c) {
-        const int t = lane & (kTok - 1);
-        const int64_t row = first + min(t, count - 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = (lane >> 4) + 4 * i;
-            const bool there = n0 + n < a.N;
-            sb[n * kTok + t] = there ? Io<T>::ld(static_cast<const T*>(a.Bm) + row * a.b_stride + n0 + n) : 0.f;
-            if constexpr (decltype(with_c)::value)
-                sc[n * kTok + t] = there ? Io<T>::ld(static_cast<const T*>(a.Cm) + row * a.c_stride + n0 + n) : 0.f;
-        }
-    };
-    // 16 tokens of one tensor, as stored; rows behind the piece are replaced by its last.  The row's address goes from token to token:
-    // computed for each, the addresses of all tokens of all tensors would fill the scalar registers
-    struct Tokens {
-        T v[kTok];
-    };
-    auto load_tokens = [&](const void* base, int64_t stride, int first, int count) {
-        const T* row = static_cast<const T*>(base) + first * stride;
-        Tokens k;
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) {
-            k.v[t] = row[d];
-            row += t + 1 < count ? stride : 0;
-        }
-        return k;
-    };
-    // step sizes and their products with u; 0 for tokens behind the piece
-    auto load_steps = [&](int first, int count, float (&dl)[kTok], float (&dx)[kTok]) {
-        const Tokens u = load_tokens(a.u, a.u_stride, first, count), delta = load_tokens(a.delta, a.d_stride, first, count);
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) dl[t] = Io<T>::ld(&delta.v[t]) + bias;
-        if (sp) corey_scan::softplus_all<kTok>(dl);
-#pragma unroll
-        for (int t = 0; t < kTok; ++t) {
-            dl[t] = t < count ? dl[t] : 0.f;
-            dx[t] = t < count ? dl[t] * Io<T>::ld(&u.v[t]) : 0.f;
-        }
+    // a state at the start of block b
+    const auto start_of = [&](int b, int n) {
+        if (b > 0) return starts[((b - 1) * kStates + n) * 64];
+        return begins ? 0.f : first_states[(int64_t)n * a.D];
     };
 
     // forward over all blocks but the last: the states that blocks 1, 2, ... begin with
-    if (blocks > 1) {
-        float h[kStates];
+    for (int b = 0; b + 1 < blocks; ++b) {
+        float dl[kTok], dx[kTok];
+        const int64_t first = p.first + (int64_t)b * kTok;
+        const float* from = bc + (int64_t)b * 2 * half;
+        float a_next = arow[0], h_next = start_of(b, 0);
+        State8 s_next[2] = {state8(from), state8(from + half)};
+        steps<T, kTok>(load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), kTok, off), load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), kTok, off),
+                       bias, sp, kTok, dl, dx);
+#pragma unroll 1
+        for (int n = 0; n < mine; ++n) {
+            const float a2 = a_next * kLog2e;
+            float h = h_next;
+            const State8 s[2] = {s_next[0], s_next[1]};
+            const int m = min(n + 1, mine - 1);
+            a_next = arow[m];
+            h_next = start_of(b, m);
+            s_next[0] = state8(from + m * 2 * kHalf);
+            s_next[1] = state8(from + m * 2 * kHalf + half);
+            float e[kTok], x[kTok];
+            arguments<kTok>(dl, a2, dx, [&](int t) { return s[t / kHalf].b(t % kHalf); }, e, x);
 #pragma unroll
-        for (int n = 0; n < kStates; ++n) h[n] = state_at_start(n);
-        for (int b = 0; b + 1 < blocks; ++b) {
-            float dl[kTok], dx[kTok];
-            lds_in_order();
-            stage_bc(p.first + b * kTok, kTok, std::false_type());
-            load_steps(p.first + b * kTok, kTok, dl, dx);
-            lds_in_order();
-#pragma unroll
-            for (int n = 0; n < kStates; ++n) {
-                float e[kTok];
-#pragma unroll
-                for (int t = 0; t < kTok; ++t) e[t] = dl[t] * a2[n];
-                exp2_burst<kTok>(e);
-                const Words<kTok> bv = words<kTok>(sb + n * kTok);
-#pragma unroll
-                for (int t = 0; t < kTok; ++t) h[n] = fmaf(e[t], h[n], dx[t] * bv.v[t]);
-                starts[(b * kStates + n) * 64] = h[n];
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int t = 0; t < kTok; ++t) h = fmaf(e[t], h, x[t]);
+            starts[(b * kStates + n) * 64] = h;
         }
     }
 
+    for (int n = 0; n < mine; ++n)
+        grads[n * 64] = on && !(p.bits & 2) ? a.backs[((int64_t)tile * a.N + safe + n) * a.D + d] : 0.f;
+    float dskip = 0.f, dbias = 0.f;
     for (int b = blocks - 1; b >= 0; --b) {
-        const int first = p.first + b * kTok, count = min(kTok, p.count - b * kTok);
+        const int64_t first = p.first + (int64_t)b * kTok;
+        const int count = min(kTok, p.count - b * kTok);
         float dl[kTok], dx[kTok], ds[kTok], gb[kTok], gk[kTok], out[kTok];
-        lds_in_order();
-        if (b == 0) {                                            // the first block's states, where block 1's were
-#pragma unroll
-            for (int n = 0; n < kStates; ++n) starts[n * 64] = state_at_start(n);
-        }
-        stage_bc(first, count, std::true_type());
-        load_steps(first, count, dl, dx);
+        const float* from = bc + (int64_t)b * 2 * half;
+        State8 s_next[2] = {state8(from), state8(from + half)};
         {
-            const Tokens dy = load_tokens(a.dy, a.dy_stride, first, count);
-            Tokens z;
-            if constexpr (GATED) z = load_tokens(a.z, a.z_stride, first, count);
+            const Tokens<T, kTok> u = load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), count, off),
+                                  delta = load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), count, off),
+                                  dy = load_tokens<T, kTok>(Rows<T>(a.dy, a.dy_stride, first), count, off);
+            if constexpr (GATED) gates<T, kTok>(load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off), ds);
+            steps<T, kTok>(u, delta, bias, sp, count, dl, dx);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) {
-                ds[t] = Io<T>::ld(&dy.v[t]);
-                if constexpr (GATED) ds[t] *= silu(Io<T>::ld(&z.v[t]));
+                ds[t] = GATED ? ds[t] * dy.at(t) : dy.at(t);
                 ds[t] = on && t < count ? ds[t] : 0.f;
                 gb[t] = gk[t] = out[t] = 0.f;
             }
         }
-        lds_in_order();
-        const float* begin = starts + max(b - 1, 0) * kStates * 64;
-#pragma unroll
-        for (int n = 0; n < kStates; ++n) {
-            float h = begin[n * 64];
+        const int64_t place = ((int64_t)group * a.blocks + block0 + b) * a.N + safe;
+        const bool fresh = b == blocks - 1;
+        float a_next = arow[0], h_next = start_of(b, 0);
+#pragma unroll 1
+        for (int n = 0; n < mine; ++n) {
+            const float a2 = a_next * kLog2e;
+            float h = h_next, gn = grads[n * 64], an = fresh ? 0.f : part[(int64_t)n * a.D];
+            const State8 s[2] = {s_next[0], s_next[1]};
+            const int m = min(n + 1, mine - 1);
+            a_next = arow[m];
+            h_next = start_of(b, m);
+            s_next[0] = state8(from + m * 2 * kHalf);
+            s_next[1] = state8(from + m * 2 * kHalf + half);
             float e[kTok], w[kTok], v[kTok];
+            arguments<kTok>(dl, a2, dx, [&](int t) { return s[t / kHalf].b(t % kHalf); }, e, v);
 #pragma unroll
-            for (int t = 0; t < kTok; ++t) e[t] = dl[t] * a2[n];
-            exp2_burst<kTok>(e);
-#pragma unroll
-            for (int q = 0; q < kTok; q += 4) {                  // (B and C four tokens at a time, and again on the way back)
-                const Words<4> bv = words<4>(sb + n * kTok + q), cv = words<4>(sc + n * kTok + q);
-#pragma unroll
-                for (int t = q; t < q + 4; ++t) {
-                    w[t] = e[t] * h;                             // a h_{t-1}
-                    h = fmaf(dx[t], bv.v[t - q], w[t]);
-                    out[t] = fmaf(cv.v[t - q], h, out[t]);
-                    v[t] = ds[t] * h;
-                }
+            for (int t = 0; t < kTok; ++t) {
+                w[t] = e[t] * h;                                 // a h_{t-1}
+                h = w[t] + v[t];
+                out[t] = fmaf(s[t / kHalf].c(t % kHalf), h, out[t]);
+                v[t] = ds[t] * h;
             }
             const float sum_c = fold16(v, lane);
-            float gn = g[n], an = dA[n];
-            asm volatile("" ::: "memory");
 #pragma unroll
-            for (int q = kTok - 4; q >= 0; q -= 4) {
-                const Words<4> bv = words<4>(sb + n * kTok + q), cv = words<4>(sc + n * kTok + q);
-#pragma unroll
-                for (int t = q + 3; t >= q; --t) {
-                    gn = fmaf(ds[t], cv.v[t - q], gn);
-                    gb[t] = fmaf(gn, bv.v[t - q], gb[t]);
-                    const float through = gn * w[t];
-                    gk[t] = fmaf(a2[n], through, gk[t]);
-                    an = fmaf(dl[t], through, an);
-                    v[t] = gn * dx[t];
-                    gn *= e[t];
-                }
+            for (int t = kTok - 1; t >= 0; --t) {
+                gn = fmaf(s[t / kHalf].c(t % kHalf), ds[t], gn);
+                gb[t] = fmaf(s[t / kHalf].b(t % kHalf), gn, gb[t]);
+                const float through = gn * w[t];
+                gk[t] = fmaf(a2, through, gk[t]);
+                an = fmaf(dl[t], through, an);
+                v[t] = gn * dx[t];
+                gn *= e[t];
             }
             const float sum_b = fold16(v, lane);
-            s_fold[wave][n * kFold + 2 * (lane >> 2) + (lane & 1)] = (lane & 1) ? sum_c : sum_b;      // (two lanes each, the same value)
-            // a state's share of the sums is added here: the compiler would rather keep all states' values and add them up at the end
-#pragma unroll
-            for (int t = 0; t < kTok; ++t) asm volatile("" : "+v"(gb[t]), "+v"(gk[t]), "+v"(out[t])::"memory");
-            asm volatile("" : "+v"(gn), "+v"(an));
-            g[n] = gn;
-            dA[n] = an;
-            __builtin_amdgcn_sched_barrier(0);
+            const float folded = (lane & 1) ? sum_c : sum_b;     // (two lanes each hold the same value for the same place)
+            const int spot = n * 2 * kTok + 2 * (lane >> 2) + (lane & 1);
+            if constexpr (GROUPS == 1) s_fold[wave][spot] = folded;
+            else a.part_bc[place * 2 * kTok + spot] = folded;
+            grads[n * 64] = gn;
+            if (on) part[(int64_t)n * a.D] = an;
         }
-        // dB and dC of the block, over the workgroup's channels
-        if constexpr (GROUPS == 1) {
+        if constexpr (GROUPS == 1) {                             // dB and dC of the block, over the workgroup's channels
             __syncthreads();
-            for (int i = (int)threadIdx.x; i < kTok * 2 * kStates; i += 64 * WAVES) {
-                const int t = i >> 5, bc = (i >> 4) & 1, n = i & (kStates - 1);
-                if (t < count && n < a.N) {
-                    float sum = 0.f;
+            for (int i = (int)threadIdx.x; i < a.N * 2 * kTok; i += 64 * WAVES) {
+                float sum = 0.f;
 #pragma unroll
-                    for (int k = 0; k < WAVES; ++k) sum += s_fold[k][n * kFold + 2 * t + bc];
-                    a.part_bc[((int64_t)group * a.ix.T + first + t) * 2 * a.N + bc * a.N + n] = sum;
-                }
+                for (int k = 0; k < WAVES; ++k) sum += s_fold[k][i];
+                a.part_bc[place * 2 * kTok + i] = sum;
             }
             __syncthreads();
-        } else {
-            lds_in_order();
-            for (int i = lane; i < kTok * 2 * kStates; i += 64) {
-                const int t = i >> 5, bc = (i >> 4) & 1, n = i & (kStates - 1);
-                if (t < count && n0 + n < a.N)
-                    a.part_bc[((int64_t)group * a.ix.T + first + t) * 2 * a.N + bc * a.N + n0 + n] = s_fold[wave][n * kFold + 2 * t + bc];
-            }
-            // the sums over the waves' states; wave 0 finishes
+        } else {                                                 // the sums over the waves' states; wave 0 finishes
             __syncthreads();
             if (wave != 0) {
 #pragma unroll
@@ -387,70 +324,72 @@ __global__ __launch_bounds__(64 * back_waves<GROUPS>(), 2) void k_packed_bwd(Pac
             }
             __syncthreads();
             if (wave != 0) continue;
-            for (int k = 1; k < GROUPS; ++k) {
+            for (int k = 0; k + 1 < GROUPS; ++k) {
 #pragma unroll
                 for (int t = 0; t < kTok; ++t) {
-                    gb[t] += s_part[k - 1][t * 64 + lane];
-                    gk[t] += s_part[k - 1][(kTok + t) * 64 + lane];
-                    out[t] += s_part[k - 1][(2 * kTok + t) * 64 + lane];
+                    gb[t] += s_part[k][t * 64 + lane];
+                    gk[t] += s_part[k][(kTok + t) * 64 + lane];
+                    out[t] += s_part[k][(2 * kTok + t) * 64 + lane];
                 }
             }
         }
         // what only the end needs is read again (from the cache): kept, it would take the registers of a state's work
-        const Tokens ku = load_tokens(a.u, a.u_stride, first, count), kd = load_tokens(a.delta, a.d_stride, first, count);
-        Tokens kz, ky;
-        if constexpr (GATED) {
-            kz = load_tokens(a.z, a.z_stride, first, count);
-            ky = load_tokens(a.dy, a.dy_stride, first, count);
-        }
-        T* du_row = static_cast<T*>(a.du) + first * a.du_stride;
-        T* dd_row = static_cast<T*>(a.ddelta) + first * a.dd_stride;
-        T* dz_row = GATED ? static_cast<T*>(a.dz) + first * a.dz_stride : nullptr;
+        const Tokens<T, kTok> u = load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), count, off),
+                              delta = load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), count, off);
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
-            const float u = Io<T>::ld(&ku.v[t]);
-            float ddl = fmaf(u, gb[t], gk[t] * kLn2);
-            if (sp) ddl *= __builtin_amdgcn_rcpf(1.f + fast_exp2(-(Io<T>::ld(&kd.v[t]) + bias) * kLog2e));
-            const float du = fmaf(skip, ds[t], dl[t] * gb[t]);
-            float dz = 0.f;
-            if constexpr (GATED) {
-                const float z = Io<T>::ld(&kz.v[t]), sig = __builtin_amdgcn_rcpf(1.f + fast_exp2(-z * kLog2e));
-                dz = Io<T>::ld(&ky.v[t]) * fmaf(skip, u, out[t]) * (sig * fmaf(z, 1.f - sig, 1.f));
-            }
-            if (on && t < count) {
-                Io<T>::st(du_row + d, du);
-                Io<T>::st(dd_row + d, ddl);
-                if constexpr (GATED) Io<T>::st(dz_row + d, dz);
-            }
-            dskip = t < count ? fmaf(ds[t], u, dskip) : dskip;
-            dbias = t < count ? dbias + ddl : dbias;
-            du_row += a.du_stride;
-            dd_row += a.dd_stride;
-            if constexpr (GATED) dz_row += a.dz_stride;
+            gk[t] = fmaf(u.at(t), gb[t], gk[t] * kLn2);
+            gb[t] = fmaf(skip, ds[t], dl[t] * gb[t]);
+            dskip = fmaf(ds[t], u.at(t), dskip);                 // (ds is 0 for tokens that are not there)
+            out[t] = fmaf(skip, u.at(t), out[t]);
+        }
+        if (on) store_tokens<T, kTok>(Rows<T>(a.du, a.du_stride, first), count, off, gb);
+        if (sp) {                                                // times sigmoid(delta + bias)
+            float sig[kTok];
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) sig[t] = -(delta.at(t) + bias) * kLog2e;
+            exp2_burst<kTok>(sig);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) sig[t] += 1.f;
+            rcp_burst<kTok>(sig);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) gk[t] *= sig[t];
+        }
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) dbias += t < count ? gk[t] : 0.f;
+        if (on) store_tokens<T, kTok>(Rows<T>(a.ddelta, a.dd_stride, first), count, off, gk);
+        if constexpr (GATED) {
+            const Tokens<T, kTok> z = load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off),
+                                  dy = load_tokens<T, kTok>(Rows<T>(a.dy, a.dy_stride, first), count, off);
+            float sig[kTok];
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) sig[t] = -z.at(t) * kLog2e;
+            exp2_burst<kTok>(sig);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) sig[t] += 1.f;
+            rcp_burst<kTok>(sig);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) out[t] *= dy.at(t) * (sig[t] * fmaf(z.at(t), 1.f - sig[t], 1.f));
+            if (on) store_tokens<T, kTok>(Rows<T>(a.dz, a.dz_stride, first), count, off, out);
         }
     }
-    if (!on) return;
-    float* part = a.part_a + (int64_t)tile * (a.N + 2) * a.D + d;
-#pragma unroll
-    for (int n = 0; n < kStates; ++n)
-        if (n0 + n < a.N) part[(int64_t)(n0 + n) * a.D] = dA[n];
-    if (n0 == 0) {
-        part[(int64_t)a.N * a.D] = dskip;
-        part[(int64_t)(a.N + 1) * a.D] = dbias;
-    }
+    if (!on || n0 != 0) return;
+    part[(int64_t)a.N * a.D] = dskip;
+    part[(int64_t)(a.N + 1) * a.D] = dbias;
 }
 
-// dB and dC: the workgroups' sums, one value a lane.
+// dB and dC: the workgroups' sums.  A lane takes one token and state of one of them.
 template <typename T> __global__ __launch_bounds__(256) void k_packed_bwd_bc(PackedScanArgs a)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, wide = 2 * a.N;
-    if (!a.ix.good() || i >= a.ix.head[4] * wide) return;
-    const int64_t t = i / wide;
-    const int j = (int)(i - t * wide);
+    const int64_t per = 2 * kTok * a.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x, block = i / per;
+    if (block >= a.blocks || !a.ix.good()) return;
+    const Piece p = a.ix.blocks[block];
+    const int j = (int)(i - block * per), t = (j >> 1) & (kTok - 1), n = j / (2 * kTok);
+    if (p.seq < 0 || t >= p.count) return;
     float sum = 0.f;
-    for (int g = 0; g < a.groups; ++g) sum += a.part_bc[(int64_t)g * a.ix.T * wide + i];
-    if (j < a.N) Io<T>::st(static_cast<T*>(a.dB) + t * a.db_stride + j, sum);
-    else Io<T>::st(static_cast<T*>(a.dC) + t * a.dc_stride + (j - a.N), sum);
+    for (int g = 0; g < a.groups; ++g) sum += a.part_bc[(int64_t)g * a.blocks * per + i];
+    if (j & 1) Io<T>::st(static_cast<T*>(a.dC) + (p.first + (int64_t)t) * a.dc_stride + n, sum);
+    else Io<T>::st(static_cast<T*>(a.dB) + (p.first + (int64_t)t) * a.db_stride + n, sum);
 }
 
 // dA, dD, dbias: the tiles' sums.  A workgroup takes 64 columns; its waves the tiles in turn.
@@ -484,18 +423,19 @@ __global__ __launch_bounds__(256) void k_packed_bwd_a(PackedScanArgs a)
 
 // The workspace's parts, in floats.
 struct Space {
-    int64_t ends, backs, sums, part_bc, part_a, all;
+    int64_t bc, ends, backs, sums, part_bc, part_a, all;
 };
 Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
 {
     const int64_t tiles = T > tile ? l.max_tiles : 0;            // (carried only where a sequence can have a second tile)
-    const int64_t groups = N <= kStates ? (D + 255) / 256 : (D + 63) / 64;
+    const int64_t groups = channel_groups(D, N);
     Space s;
-    s.ends = 0;
+    s.bc = 0;
+    s.ends = s.bc + l.max_blocks * N * 32 + 32;                  // (the loop over the states asks for one more than there is)
     s.backs = s.ends + tiles * N * D;
     s.sums = s.backs + tiles * N * D;
     s.part_bc = s.sums + tiles * D;
-    s.part_a = s.part_bc + groups * T * 2 * N;
+    s.part_a = s.part_bc + groups * l.max_blocks * 32 * N;
     s.all = s.part_a + l.max_tiles * (N + 2) * D;
     return s;
 }
@@ -552,13 +492,14 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
     a.du = du; a.ddelta = ddelta; a.dz = dz; a.dB = dB; a.dC = dC;
     a.du_stride = du_stride; a.dd_stride = ddelta_stride; a.dz_stride = dz_stride; a.db_stride = dB_stride; a.dc_stride = dC_stride;
     a.dA = dA; a.dD = dDv; a.dbias = ddelta_bias;
-    a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
+    a.bc = ws + w.bc; a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
     a.D = (int32_t)D; a.N = (int32_t)N;
     a.softplus = delta_softplus ? 1 : 0;
-    a.tiles = (int32_t)l.max_tiles;
-    const int64_t pairs = (D + 127) / 128, columns = (D * N + 255) / 256, groups = N <= kStates ? (D + 255) / 256 : (D + 63) / 64;
-    const int64_t bc = (pack->T * 2 * N + 255) / 256;
-    if (l.max_tiles * groups > INT32_MAX || l.max_tiles * pairs > INT32_MAX || 2 * columns * (l.max_longs + 1) > INT32_MAX || bc > INT32_MAX)
+    a.blocks = (int32_t)l.max_blocks;
+    a.groups = (int32_t)channel_groups(D, N);
+    const int64_t columns = (D * N + 255) / 256, groups = channel_groups(D, N);
+    const int64_t relay = (l.max_blocks * N * 32 + 255) / 256;
+    if (l.max_tiles * groups > INT32_MAX || 2 * columns * (l.max_longs + 1) > INT32_MAX || relay > INT32_MAX)
         return fail(COREY_ESHAPE, "%s: T * D is too large", who);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     hipError_t attr = hipSuccess;
@@ -566,27 +507,28 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
         using T = decltype(t);
         by_groups(N, [&](auto gr) {
             constexpr int G = decltype(gr)::value;
-            auto go = [&](auto gate) {
+            const auto go = [&](auto gate, auto whole) {
                 constexpr bool Z = decltype(gate)::value;
-                const size_t lds = (size_t)back_waves<G>() * (size_t)start_slots(pack->tile) * kStates * 64 * 4;
+                const size_t lds = (size_t)Shape<G>::waves * (size_t)kept(pack->tile) * kStates * 64 * 4;
                 // (what the longest tile takes, whatever this call's: another thread's call may be between this line and its launch)
-                constexpr int most = back_waves<G>() * start_slots(G == 8 ? 32 : kMaxBackTile) * kStates * 64 * 4;
+                constexpr int most = Shape<G>::waves * kept(G == 8 ? 32 : kMaxBackTile) * kStates * 64 * 4;
                 attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_packed_bwd<T, Z, G>), hipFuncAttributeMaxDynamicSharedMemorySize, most);
                 if (attr != hipSuccess) return;
+                k_packed_relay<T><<<(unsigned)relay, 256, 0, stream>>>(a);
                 if (pack->T > pack->tile) {
-                    a.groups = (int32_t)pairs;
-                    const unsigned grid = (unsigned)(l.max_tiles * pairs);
-                    if (D % 2 == 0) k_packed_bwd_ends<T, true, Z, G><<<grid, 64 * G, 0, stream>>>(a);
-                    else k_packed_bwd_ends<T, false, Z, G><<<grid, 64 * G, 0, stream>>>(a);
+                    k_packed_bwd_ends<T, Z, G, decltype(whole)::value><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
                     k_packed_bwd_chain<<<(unsigned)(2 * columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
                 }
-                a.groups = (int32_t)groups;
-                k_packed_bwd<T, Z, G><<<(unsigned)(l.max_tiles * groups), 64 * back_waves<G>(), lds, stream>>>(a);
+                k_packed_bwd<T, Z, G><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, lds, stream>>>(a);
             };
-            if (z) go(std::true_type());
-            else go(std::false_type());
+            const auto with = [&](auto gate) {
+                if (N == G * kStates) go(gate, std::true_type());
+                else go(gate, std::false_type());
+            };
+            if (z) with(std::true_type());
+            else with(std::false_type());
         });
-        if (attr == hipSuccess) k_packed_bwd_bc<T><<<(unsigned)bc, 256, 0, stream>>>(a);
+        if (attr == hipSuccess) k_packed_bwd_bc<T><<<(unsigned)relay, 256, 0, stream>>>(a);
     });
     if (attr != hipSuccess) return corey::hip_fail(attr, "corey_scan_packed_bwd: LDS");
     k_packed_bwd_a<<<(unsigned)(((N + 2) * D + 63) / 64), 256, 0, stream>>>(a);
