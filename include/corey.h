@@ -445,7 +445,7 @@ typedef struct {
 /* corey_pack_plan -- builds the index on the GPU from the sequences' lengths, without a host round trip.
  *   lengths     DEVICE int32[S], 1 <= S <= COREY_PACK_MAX_SEQS.  Lengths below 0 count as 0; sequences that do not fit into T rows
  *               are cut off there.       T: rows of the batch's tensors, 1 <= T < 2^31.
- *   tile        power of two in [COREY_PACK_BLOCK, COREY_PACK_MAX_TILE]: tokens of a sequence that the scan walks in one go
+ *   tile        a multiple of COREY_PACK_BLOCK up to COREY_PACK_MAX_TILE: tokens of a sequence that the scan walks in one go
  *               (corey_pack_tile gives a good one).  The results do not depend on it beyond reassociation.
  *   table       DEVICE, corey_pack_bytes(S, T, tile) bytes, 16-byte aligned.  int32 words: a head of 16 (words 4 .. 7: tokens, tiles,
  *               blocks in use, sequences of more than one tile); starts[S + 1], the row each sequence begins at and the end;

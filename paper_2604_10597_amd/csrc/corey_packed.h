@@ -17,6 +17,9 @@ struct __align__(16) Piece {
     int32_t seq, first, count, bits;
 };
 
+// Tiles are whole blocks.
+inline bool good_tile(int32_t tile) { return tile >= COREY_PACK_BLOCK && tile <= COREY_PACK_MAX_TILE && tile % COREY_PACK_BLOCK == 0; }
+
 // Word offsets of the index's parts.
 struct Layout {
     int64_t starts, seq, tiles, blocks, tile_begin, block_begin, longs, words, max_tiles, max_blocks, max_longs;
@@ -60,8 +63,7 @@ inline int index_of(const char* who, const corey_pack* p, Index* ix)
 {
     using corey::fail;
     if (!p || !p->table) return fail(COREY_ENULL, "%s: the index is NULL (corey_pack_plan fills it)", who);
-    if (p->S < 1 || p->T < 1 || p->T > INT32_MAX || p->S > COREY_PACK_MAX_SEQS || !corey::is_pow2(p->tile) || p->tile < COREY_PACK_BLOCK ||
-        p->tile > COREY_PACK_MAX_TILE)
+    if (p->S < 1 || p->T < 1 || p->T > INT32_MAX || p->S > COREY_PACK_MAX_SEQS || !good_tile(p->tile))
         return fail(COREY_EINVAL, "%s: the index was not filled by corey_pack_plan", who);
     const Layout l = layout(p->S, p->T, p->tile);
     if (p->bytes < (size_t)l.words * 4 || reinterpret_cast<uintptr_t>(p->table) % 16 != 0)

@@ -26,7 +26,7 @@ struct PlanArgs {
     const int32_t* lengths;
     int32_t *head, *starts, *seq, *tile_begin, *block_begin, *longs;
     Piece *tiles, *blocks;
-    int32_t S, T, tile, tile_log2;
+    int32_t S, T, tile;
     int32_t max_tiles, max_blocks;
     int32_t token_groups, tile_groups;    // workgroups for the tokens, for the tiles; the rest are for the blocks
 };
@@ -89,7 +89,7 @@ __device__ Sums sum_up(const PlanArgs& a, int s0, int n, Sums before, int32_t* s
         const uint32_t next = add_capped(at, len[i], cap);
         if (first + i < n) starts[first + i] = (int32_t)at;
         len[i] = next - at;                                     // what of it fits
-        nt += (len[i] + a.tile - 1) >> a.tile_log2;
+        nt += (len[i] + a.tile - 1) / (uint32_t)a.tile;
         nb += (len[i] + kBlock - 1) / kBlock;
         nl += len[i] > (uint32_t)a.tile;
         at = next;
@@ -112,7 +112,7 @@ __device__ Sums sum_up(const PlanArgs& a, int s0, int n, Sums before, int32_t* s
                 ++lb;
             }
         }
-        tb += (len[i] + a.tile - 1) >> a.tile_log2;
+        tb += (len[i] + a.tile - 1) / (uint32_t)a.tile;
         bb += (len[i] + kBlock - 1) / kBlock;
     }
     if (threadIdx.x == 0) {
@@ -136,16 +136,16 @@ __device__ __forceinline__ int holder(const int32_t* begin, int S, int i)
     return lo;
 }
 
-__device__ void fill_pieces(const int32_t* starts, const int32_t* begin, int S, int size_log2, Piece* out, int i, int room)
+__device__ void fill_pieces(const int32_t* starts, const int32_t* begin, int S, int size, Piece* out, int i, int room)
 {
     if (i >= room) return;
     Piece p{-1, 0, 0, 0};
     if (i < begin[S]) {
         const int s = holder(begin, S, i), k = i - begin[s];
-        const int n = starts[s + 1] - starts[s], at = k << size_log2;
+        const int n = starts[s + 1] - starts[s], at = k * size;
         p.seq = s;
         p.first = starts[s] + at;
-        p.count = min(n - at, 1 << size_log2);
+        p.count = min(n - at, size);
         p.bits = (k == 0 ? 1 : 0) + (i + 1 == begin[s + 1] ? 2 : 0);
     }
     out[i] = p;
@@ -178,8 +178,8 @@ __device__ void fill(const PlanArgs& a, const int32_t* starts, const int32_t* ti
         return;
     }
     g -= a.token_groups;
-    if (g < a.tile_groups) fill_pieces(starts, tile_begin, a.S, a.tile_log2, a.tiles, g * kThreads + (int)threadIdx.x, a.max_tiles);
-    else fill_pieces(starts, block_begin, a.S, 4, a.blocks, (g - a.tile_groups) * kThreads + (int)threadIdx.x, a.max_blocks);
+    if (g < a.tile_groups) fill_pieces(starts, tile_begin, a.S, a.tile, a.tiles, g * kThreads + (int)threadIdx.x, a.max_tiles);
+    else fill_pieces(starts, block_begin, a.S, kBlock, a.blocks, (g - a.tile_groups) * kThreads + (int)threadIdx.x, a.max_blocks);
 }
 
 __device__ void write_head(const PlanArgs& a, const Sums& all)
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void k_pack_fill(PlanArgs a) { fill(a, a.
 
 extern "C" size_t corey_pack_bytes(int64_t S, int64_t T, int32_t tile)
 {
-    if (S < 1 || S > COREY_PACK_MAX_SEQS || T < 1 || T > INT32_MAX || !corey::is_pow2(tile) || tile < COREY_PACK_BLOCK || tile > COREY_PACK_MAX_TILE)
+    if (S < 1 || S > COREY_PACK_MAX_SEQS || T < 1 || T > INT32_MAX || !good_tile(tile))
         return 0;
     return (size_t)layout(S, T, tile).words * 4;
 }
@@ -236,8 +236,8 @@ extern "C" int corey_pack_plan(const int32_t* lengths, int64_t S, int64_t T, int
     if (!lengths || !table || !pack) return fail(COREY_ENULL, "corey_pack_plan: lengths, table and pack are required");
     if (S < 1 || S > COREY_PACK_MAX_SEQS) return fail(COREY_ESHAPE, "corey_pack_plan: 1 <= S <= %d required", COREY_PACK_MAX_SEQS);
     if (T < 1 || T > INT32_MAX) return fail(COREY_ESHAPE, "corey_pack_plan: 1 <= T < 2^31 required");
-    if (!corey::is_pow2(tile) || tile < COREY_PACK_BLOCK || tile > COREY_PACK_MAX_TILE)
-        return fail(COREY_EINVAL, "corey_pack_plan: tile must be a power of two in [%d, %d]", COREY_PACK_BLOCK, COREY_PACK_MAX_TILE);
+    if (!good_tile(tile))
+        return fail(COREY_EINVAL, "corey_pack_plan: tile must be a multiple of %d up to %d", COREY_PACK_BLOCK, COREY_PACK_MAX_TILE);
     const Layout l = layout(S, T, tile);
     if (table_bytes < (size_t)l.words * 4 || reinterpret_cast<uintptr_t>(table) % 16 != 0)
         return fail(COREY_EWORKSPACE, "corey_pack_plan: table must be 16-byte aligned and have corey_pack_bytes() bytes");
@@ -255,7 +255,6 @@ extern "C" int corey_pack_plan(const int32_t* lengths, int64_t S, int64_t T, int
     a.S = (int32_t)S;
     a.T = (int32_t)T;
     a.tile = tile;
-    a.tile_log2 = __builtin_ctz((unsigned)tile);
     a.max_tiles = (int32_t)l.max_tiles;
     a.max_blocks = (int32_t)l.max_blocks;
     const auto groups = [](int64_t n, int64_t per) { return (int32_t)((n + per - 1) / per); };

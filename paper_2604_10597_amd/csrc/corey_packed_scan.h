@@ -40,6 +40,7 @@ struct PackedScanArgs {
     float *dA, *dD, *dbias;
     int64_t dy_stride, du_stride, dd_stride, dz_stride, db_stride, dc_stride;
     float* backs;                         // workspace [tiles, N, D]: what a tile hands to the gradient of the state it begins with
+    float* starts;                        // workspace [tiles, tile / 16 - 1, N, D]: the states that a tile's blocks 1, 2, ... begin with
     float* part_bc;                       // workspace [channel groups, blocks, N, 16 tokens, (dB, dC)]
     float* part_a;                        // workspace [tiles, N + 2, D]: dA, dD and dbias of a tile
 };
@@ -76,6 +77,26 @@ __device__ __forceinline__ State8 state8(const float* p)
     s.v = *(const __attribute__((address_space(4))) State8::Vec*)(uintptr_t)p;
     return s;
 }
+
+// States n and n + 1 of a wave, and the two behind them on their way: scalar loads come back in any order, so a wait for one is a wait
+// for all, and each pair is asked for two states of work ahead.
+struct StatePairs {
+    State8 s[2][2];
+    const float* from;
+    __device__ __forceinline__ explicit StatePairs(const float* p) : from(p)
+    {
+        s[0][0] = state8(from);
+        s[0][1] = state8(from + 2 * kHalf);
+    }
+    __device__ __forceinline__ const State8& at(int n) const { return s[(n >> 1) & 1][n & 1]; }
+    // at the start of state n's work (behind the wave's last states: the next block's, or the workspace's end)
+    __device__ __forceinline__ void ahead(int n)
+    {
+        if ((n & 1) != 0 || n + 2 >= kStates) return;
+        s[((n >> 1) + 1) & 1][0] = state8(from + (n + 2) * 2 * kHalf);
+        s[((n >> 1) + 1) & 1][1] = state8(from + (n + 3) * 2 * kHalf);
+    }
+};
 
 // The blocks a tile's tokens lie in: the number of the first.
 __device__ __forceinline__ int64_t first_block(const Index& ix, const Piece& p) { return ix.block_begin[p.seq] + (p.first - ix.starts[p.seq]) / kBlock; }

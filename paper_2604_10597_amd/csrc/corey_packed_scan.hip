@@ -48,9 +48,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_ends(Pa
     const float bias = a.bias ? a.bias[d] : 0.f;
     const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + n0) * 2 * kHalf;
     for (int t0 = 0; t0 < p.count; t0 += K) {                    // (a tile that is not its sequence's last is whole)
-        State8 s[3];                                             // two states ahead
-        s[0] = state8(from);
-        s[1] = state8(from + 2 * kHalf);
+        StatePairs s(from);
         float dl[K], dx[K];
         steps<T, K>(u, delta, bias, a.softplus != 0, K, dl, dx);
         const int left = p.count - t0 - K, on = left > 0 ? K : 0;  // (behind the last block: the same rows again, for nothing)
@@ -63,9 +61,9 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_ends(Pa
 #pragma unroll
         for (int n = 0; n < kStates; ++n) {
             if (!WHOLE && n0 + n >= a.N) continue;
-            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);
+            s.ahead(n);
             float e[K], x[K];
-            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s.at(n).b(t); }, e, x);
 #pragma unroll
             for (int t = 0; t < K; ++t) h[n] = fmaf(e[t], h[n], x[t]);
             __builtin_amdgcn_sched_barrier(0);
@@ -149,9 +147,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_scan(Pa
     const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + (states ? n0 : 0)) * 2 * kHalf;
     for (int t0 = 0; t0 < p.count; t0 += K) {
         const int count = p.count - t0;
-        State8 s[3];                                             // two states ahead
-        s[0] = state8(from);
-        s[1] = state8(from + 2 * kHalf);
+        StatePairs s(from);
         float dl[K], dx[K], acc[K];
         Tokens<T, K> z;                                          // (needed at the end: requested now, not with the block before)
         if constexpr (GATED) {
@@ -169,13 +165,13 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_scan(Pa
 #pragma unroll
         for (int n = 0; n < kStates; ++n) {
             if (!WHOLE && n0 + n >= a.N) continue;
-            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);   // (behind the last: the next block's, or the end's)
+            s.ahead(n);
             float e[K], x[K];
-            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s.at(n).b(t); }, e, x);
 #pragma unroll
             for (int t = 0; t < K; ++t) {
                 h[n] = fmaf(e[t], h[n], x[t]);
-                acc[t] = fmaf(s[n % 3].c(t), h[n], acc[t]);
+                acc[t] = fmaf(s.at(n).c(t), h[n], acc[t]);
                 // a state's share of the sums is added here: left to itself the compiler moves a token's sum over the states into the
                 // branch that stores it, and keeps the states of all tokens until then
                 asm volatile("" : "+v"(acc[t]), "+v"(h[n]));
@@ -309,17 +305,30 @@ __global__ __launch_bounds__(256) void k_packed_step(StepArgs a)
 
 }  // namespace
 
-// Tiles are what runs side by side: about four waves a SIMD fill the GPU (4096 of 64 channels and 16 states).  Longer tiles than
-// that needs mean fewer begun states to form and to carry, and none at all for the sequences that fit into one.
+// Tiles are what runs side by side: some 4.5 waves of 64 channels and 16 states a SIMD, and half a tile a sequence for the ends that fill
+// none.  Shorter tiles mean more begun states to form and to carry, longer ones idle SIMDs (one sequence of 16384 tokens, 5120 channels:
+// tiles of 64, 128, 192 ... 320, 512, 1024 tokens 553, 459, 455, 543, 777 us).  With many sequences a tile takes whole ones and nothing
+// is begun.
 extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
 {
     if (S < 1 || T < 1 || D < 1 || N < 1) return 0;
     const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16);
-    const double most = (double)T * waves / 4096.0;
-    const int32_t longest = !backward ? 1024 : N > 64 ? 32 : 64;
-    int32_t tile = COREY_PACK_BLOCK;
-    while (tile < longest && 2 * tile <= most) tile *= 2;
-    return tile;
+    if (backward) {
+        // a tile's work is in proportion to its tokens and some for each tile; three waves a SIMD run at once, and a round lasts as long as a
+        // tile.  8192 tokens of 2048 channels in 11 sequences: 16, 32, 48, 64 tokens 459, 417, 403, 445 us; 2048 of 1536 116, 128, 163, 168
+        int32_t best = 0;
+        double least = 0.;
+        for (int32_t tile = COREY_PACK_BLOCK; tile <= (N > 64 ? 32 : 64); tile += COREY_PACK_BLOCK) {
+            double rounds = (double)(int64_t)(((double)T / tile + 0.5 * (double)S) * waves / 3072.0 + 0.9);
+            if (rounds < 1.) rounds = 1.;
+            const double cost = rounds * (tile + 8);
+            if (best == 0 || cost < least) best = tile, least = cost;
+        }
+        return best;
+    }
+    const double fit = 4608.0 / waves, room = fit - 0.5 * (double)S, tile = room >= 1.0 ? (double)T / room : 1024.0;
+    if (tile >= 1024.0) return 1024;
+    return ((int32_t)tile / COREY_PACK_BLOCK + 1) * COREY_PACK_BLOCK;
 }
 
 namespace {
@@ -332,7 +341,7 @@ Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
     const int64_t tiles = T > tile ? l.max_tiles : 0;            // (carried only where a sequence can have a second tile)
     Space s;
     s.bc = 0;
-    s.ends = s.bc + l.max_blocks * N * 32 + 32;                  // (the loop over the states asks for two more than there are)
+    s.ends = s.bc + l.max_blocks * N * 32 + 48;                  // (the loop over the states asks for three more than there are)
     s.sums = s.ends + tiles * N * D;
     s.all = s.sums + tiles * D;
     return s;

@@ -65,9 +65,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
     const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + n0) * 2 * kHalf;
     for (int t0 = 0; t0 < p.count; t0 += K) {
         const int count = p.count - t0;
-        State8 s[3];                                             // two states ahead
-        s[0] = state8(from);
-        s[1] = state8(from + 2 * kHalf);
+        StatePairs s(from);
         float dl[K], dx[K], ds[K];
         steps<T, K>(u, delta, bias, a.softplus != 0, count, dl, dx);
         if constexpr (GATED) gates<T, K>(z, ds);
@@ -83,14 +81,14 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
 #pragma unroll
         for (int n = 0; n < kStates; ++n) {
             if (!WHOLE && n0 + n >= a.N) continue;
-            if (n + 2 < kStates) s[(n + 2) % 3] = state8(from + (n + 2) * 2 * kHalf);   // (behind the last: the next block's, or the end's)
+            s.ahead(n);
             float e[K], x[K], g = 0.f;
-            arguments<K>(dl, a2[n], dx, [&](int t) { return s[n % 3].b(t); }, e, x);
+            arguments<K>(dl, a2[n], dx, [&](int t) { return s.at(n).b(t); }, e, x);
 #pragma unroll
             for (int t = 0; t < K; ++t) {
                 h[n] = fmaf(e[t], h[n], x[t]);
                 const int r = K - 1 - t;                         // (and the gradients from the last token back)
-                g = fmaf(s[n % 3].c(r), ds[r], g) * e[r];
+                g = fmaf(s.at(n).c(r), ds[r], g) * e[r];
             }
             back[n] = fmaf(fast_exp2(before * a2[n]), g, back[n]);
             __builtin_amdgcn_sched_barrier(0);
@@ -144,46 +142,60 @@ __global__ __launch_bounds__(256) void k_packed_bwd_chain(PackedScanArgs a, int 
     }
 }
 
-// 16 values of every lane, summed over the wave's 64 lanes: every lane leaves with the sum of value lane / 4.  Halving: lanes of one
-// half hand over the values that the other half sums.  Across 32 and 16 lanes the swap instructions bring both halves' parts of two
-// values into place at once; below, DPP.
-__device__ __forceinline__ float fold16(float (&v)[16], int lane)
+// Sums of 16 values of every lane over the wave's 64 lanes, by way of LDS: a value's 64 parts are a row there, four lanes add up a
+// quarter of it each and then their sums.  (Halving over lanes in registers takes 24 swaps and selects of 8 and 4 cycles a fold where
+// this takes 15 additions and 2 DPP additions; and an eighth of the LDS unit's time.)  The row's length keeps the reads of 16 bytes from
+// meeting in the same banks.  The LDS unit takes a wave's accesses in order, so nothing waits between a lane's write and another's
+// read; the compiler is held to the order.
+constexpr int kFoldRow = 68, kFoldRows = kTok * kFoldRow;
+__device__ __forceinline__ void lds_in_order()
 {
-    auto swap_add = [](float& x, float y, auto swap) {
-        const auto r = swap(__float_as_uint(x), __float_as_uint(y));
-        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    };
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+__device__ __forceinline__ void fold_put(float* buf, const float (&v)[kTok], int lane)
+{
+    lds_in_order();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) swap_add(v[i], v[i + 8], [](uint32_t x, uint32_t y) { return __builtin_amdgcn_permlane32_swap(x, y, false, false); });
+    for (int t = 0; t < kTok; ++t) buf[t * kFoldRow + lane] = v[t];
+    lds_in_order();
+}
+struct Quarter {                          // of the row of value lane / 4
+    corey_scan::float4v v[4];
+};
+__device__ __forceinline__ Quarter fold_read(const float* buf, int lane)
+{
+    const corey_scan::float4v* row = reinterpret_cast<const corey_scan::float4v*>(buf + (lane >> 2) * kFoldRow + (lane & 3) * 16);
+    Quarter q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) swap_add(v[i], v[i + 4], [](uint32_t x, uint32_t y) { return __builtin_amdgcn_permlane16_swap(x, y, false, false); });
-    constexpr int kXor8 = 0x128, kMirror8 = 0x141, kXor2 = 0x4e, kXor1 = 0xb1;     // row_ror:8, row_half_mirror, quad_perm
-    const bool b3 = (lane & 8) != 0, b2 = (lane & 4) != 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float keep = b3 ? v[i + 2] : v[i], send = b3 ? v[i] : v[i + 2];
-        v[i] = keep + dpp_move<kXor8>(send);
-    }
-    const float keep = b2 ? v[1] : v[0], send = b2 ? v[0] : v[1];
-    float r = keep + dpp_move<kMirror8>(send);
+    for (int i = 0; i < 4; ++i) q.v[i] = row[i];
+    return q;
+}
+// every lane leaves with the sum of value lane / 4
+__device__ __forceinline__ float fold_sum(const Quarter& q)
+{
+    const corey_scan::float4v a = q.v[0] + q.v[1], b = q.v[2] + q.v[3], c = a + b;
+    float r = (c[0] + c[1]) + (c[2] + c[3]);
+    constexpr int kXor2 = 0x4e, kXor1 = 0xb1;                    // quad_perm
     r += dpp_move<kXor2>(r);
     r += dpp_move<kXor1>(r);
     return r;
 }
 
-// Values of a wave's states that it keeps in LDS, per lane: at the starts of blocks 1, 2, ... (a slot each), and the gradients.
-__host__ __device__ constexpr int kept(int tile) { return tile / kTok; }
-
 // The loop over the states is a loop (unrolled it is 50 KB of instructions, more than the instruction cache feeds), so what belongs to
-// a state from block to block stays out of registers: its value at the starts of the blocks and its gradient in LDS, its share of dA
-// in the workspace, where each lane adds to its own.
+// a state from block to block stays out of registers: its gradient and its share of dA in LDS, per lane, and its value at the starts
+// of the blocks in the workspace (in LDS it would halve the waves of a SIMD).
 template <typename T, bool GATED, int GROUPS>
 __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(PackedScanArgs a)
 {
     constexpr int WAVES = Shape<GROUPS>::waves;
-    __shared__ float s_fold[GROUPS == 1 ? WAVES : 1][GROUPS == 1 ? kStates * 2 * kTok : 1];
-    __shared__ float s_part[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? 3 * kTok * 64 : 1];
-    extern __shared__ float s_kept[];     // [WAVES][kept(tile)][16 states][64 lanes]
+    // Per wave: rows of values being folded (GROUPS > 1: then its sums over its states), gradients (forward: states), shares of dA, and
+    // folded sums.  With 128 states that is all the LDS there is.
+    constexpr int kRows = GROUPS > 1 ? 3 * kTok * 64 : 2 * kFoldRows, kKept = kStates * 64, kFolded = GROUPS == 1 ? kStates * 2 * kTok : 0;
+    static_assert(kRows >= 2 * kFoldRows && kRows % 4 == 0 && kKept % 4 == 0 && kFolded % 4 == 0, "rows are read 16 bytes at a time");
+    __shared__ __align__(16) float s_mem[WAVES][kRows + 2 * kKept + kFolded];
+    static_assert(sizeof(s_mem) <= 160 * 1024, "a compute unit's LDS");
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
     const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups), group = (int)(blockIdx.x % (unsigned)a.groups);
@@ -202,89 +214,133 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
     const int half = a.N * 2 * kHalf;                            // from one half of a block to the next
     const float* arow = a.A + (int64_t)d * a.N + safe;
     const float* first_states = a.ends + ((int64_t)tile * a.N + safe) * a.D + d;
+    const int64_t slab = (int64_t)a.N * a.D;
+    float* starts = a.starts + ((int64_t)tile * (a.ix.tile / kTok - 1) * a.N + safe) * a.D + d;
     float* part = a.part_a + ((int64_t)tile * (a.N + 2) + safe) * a.D + d;
     const bool begins = (p.bits & 1) != 0;                       // the sequence begins here, from zero
-    float* starts = s_kept + (int64_t)wave * kept(a.ix.tile) * kStates * 64 + lane;
-    float* grads = starts + (kept(a.ix.tile) - 1) * kStates * 64;
+    float* rows = s_mem[wave];
+    float* grads = rows + kRows + lane;
+    float* shares = grads + kKept;
+    constexpr int kFoldAt = kRows + 2 * kKept;
     const int blocks = (p.count + kTok - 1) / kTok;
-    // a state at the start of block b
-    const auto start_of = [&](int b, int n) {
-        if (b > 0) return starts[((b - 1) * kStates + n) * 64];
-        return begins ? 0.f : first_states[(int64_t)n * a.D];
-    };
 
-    // forward over all blocks but the last: the states that blocks 1, 2, ... begin with
-    for (int b = 0; b + 1 < blocks; ++b) {
-        float dl[kTok], dx[kTok];
+    // The next block's tokens are asked for ahead of a block's loop over the states (forward) or of its last part (backward).
+    Tokens<T, kTok> u, delta, dy, z;
+    const auto request = [&](int b, int count) {
         const int64_t first = p.first + (int64_t)b * kTok;
-        const float* from = bc + (int64_t)b * 2 * half;
-        float a_next = arow[0], h_next = start_of(b, 0);
-        State8 s_next[2] = {state8(from), state8(from + half)};
-        steps<T, kTok>(load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), kTok, off), load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), kTok, off),
-                       bias, sp, kTok, dl, dx);
-#pragma unroll 1
-        for (int n = 0; n < mine; ++n) {
-            const float a2 = a_next * kLog2e;
-            float h = h_next;
-            const State8 s[2] = {s_next[0], s_next[1]};
-            const int m = min(n + 1, mine - 1);
-            a_next = arow[m];
-            h_next = start_of(b, m);
-            s_next[0] = state8(from + m * 2 * kHalf);
-            s_next[1] = state8(from + m * 2 * kHalf + half);
-            float e[kTok], x[kTok];
-            arguments<kTok>(dl, a2, dx, [&](int t) { return s[t / kHalf].b(t % kHalf); }, e, x);
+        u = load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), count, off);
+        delta = load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), count, off);
+    };
+    const auto request_rest = [&](int b, int count) {
+        const int64_t first = p.first + (int64_t)b * kTok;
+        dy = load_tokens<T, kTok>(Rows<T>(a.dy, a.dy_stride, first), count, off);
+        if constexpr (GATED) z = load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off);
+    };
+    const int last_count = p.count - (blocks - 1) * kTok;
+    request(0, blocks > 1 ? kTok : last_count);
+
+    // forward over all blocks but the last: the states that blocks 1, 2, ... begin with.  (A log2(e) lies where rows are folded later: a
+    // global load in this loop would be waited for together with the next block's tokens.)
+    if (blocks > 1) {
+        float* decays = rows + lane;
+        float row[kStates];
+        load_row<kStates>(row, arow, safe, a.N);
 #pragma unroll
-            for (int t = 0; t < kTok; ++t) h = fmaf(e[t], h, x[t]);
-            starts[(b * kStates + n) * 64] = h;
+        for (int n = 0; n < kStates; ++n) decays[n * 64] = row[n] * kLog2e;
+#pragma unroll 4
+        for (int n = 0; n < mine; ++n) grads[n * 64] = begins ? 0.f : first_states[(int64_t)n * a.D];
+        for (int b = 0; b + 1 < blocks; ++b) {
+            float dl[kTok], dx[kTok];
+            const float* from = bc + (int64_t)b * 2 * half;
+            float a_next = decays[0];
+            State8 s_next[2] = {state8(from), state8(from + half)};
+            steps<T, kTok>(u, delta, bias, sp, kTok, dl, dx);
+            request(b + 1, b + 2 < blocks ? kTok : last_count);
+#pragma unroll 1
+            for (int n = 0; n < mine; ++n) {
+                const int m = min(n + 1, mine - 1);
+                const float a2 = a_next;
+                a_next = decays[m * 64];
+                float h = grads[n * 64];
+                float e[kTok];
+#pragma unroll
+                for (int t = 0; t < kTok; ++t) e[t] = dl[t] * a2;
+                __builtin_amdgcn_sched_barrier(0);
+                exp2_burst<kTok>(e);
+                __builtin_amdgcn_sched_barrier(0);
+                const State8 s[2] = {s_next[0], s_next[1]};
+                s_next[0] = state8(from + m * 2 * kHalf);
+                s_next[1] = state8(from + m * 2 * kHalf + half);
+#pragma unroll
+                for (int t = 0; t < kTok; ++t) h = fmaf(e[t], h, dx[t] * s[t / kHalf].b(t % kHalf));
+                grads[n * 64] = h;
+                if (on) starts[b * slab + (int64_t)n * a.D] = h;
+            }
         }
     }
+    request_rest(blocks - 1, last_count);
 
-    for (int n = 0; n < mine; ++n)
+#pragma unroll 4
+    for (int n = 0; n < mine; ++n) {
         grads[n * 64] = on && !(p.bits & 2) ? a.backs[((int64_t)tile * a.N + safe + n) * a.D + d] : 0.f;
+        shares[n * 64] = 0.f;
+    }
     float dskip = 0.f, dbias = 0.f;
     for (int b = blocks - 1; b >= 0; --b) {
         const int64_t first = p.first + (int64_t)b * kTok;
         const int count = min(kTok, p.count - b * kTok);
+        const int next = max(b - 1, 0), next_count = b > 0 ? kTok : count;       // (behind the first block: the same rows again, for nothing)
         float dl[kTok], dx[kTok], ds[kTok], gb[kTok], gk[kTok], out[kTok];
         const float* from = bc + (int64_t)b * 2 * half;
         State8 s_next[2] = {state8(from), state8(from + half)};
-        {
-            const Tokens<T, kTok> u = load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), count, off),
-                                  delta = load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), count, off),
-                                  dy = load_tokens<T, kTok>(Rows<T>(a.dy, a.dy_stride, first), count, off);
-            if constexpr (GATED) gates<T, kTok>(load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off), ds);
-            steps<T, kTok>(u, delta, bias, sp, count, dl, dx);
+        if constexpr (GATED) gates<T, kTok>(z, ds);
+        steps<T, kTok>(u, delta, bias, sp, count, dl, dx);
 #pragma unroll
-            for (int t = 0; t < kTok; ++t) {
-                ds[t] = GATED ? ds[t] * dy.at(t) : dy.at(t);
-                ds[t] = on && t < count ? ds[t] : 0.f;
-                gb[t] = gk[t] = out[t] = 0.f;
-            }
+        for (int t = 0; t < kTok; ++t) {
+            ds[t] = GATED ? ds[t] * dy.at(t) : dy.at(t);
+            ds[t] = on && t < count ? ds[t] : 0.f;
+            gb[t] = gk[t] = out[t] = 0.f;
         }
         const int64_t place = ((int64_t)group * a.blocks + block0 + b) * a.N + safe;
-        const bool fresh = b == blocks - 1;
-        float a_next = arow[0], h_next = start_of(b, 0);
+        // the states the block begins with
+        const float* begin = b > 0 ? starts + (b - 1) * slab : first_states;
+        const bool zero = b == 0 && begins;
+        float a_next = arow[0], h_next = zero ? 0.f : begin[0];
+        // a token's sums of dB and dC of state n: four lanes hold both, the even ones put the first in its place, the odd ones the second
+        const auto put_fold = [&](int n, float sum_b, float sum_c) {
+            const float sum = (lane & 1) ? sum_c : sum_b;
+            const int spot = n * 2 * kTok + 2 * (lane >> 2) + (lane & 1);
+            if constexpr (GROUPS == 1) s_mem[wave][kFoldAt + spot] = sum;
+            else a.part_bc[place * 2 * kTok + spot] = sum;
+        };
 #pragma unroll 1
         for (int n = 0; n < mine; ++n) {
+            // What LDS has for this state and the folded rows of the one before are asked for ahead of the exponentials; behind them
+            // comes the wait for all of it and for the scalar loads (they count together), and then the next scalar loads go out.
             const float a2 = a_next * kLog2e;
-            float h = h_next, gn = grads[n * 64], an = fresh ? 0.f : part[(int64_t)n * a.D];
+            float h = h_next, gn = grads[n * 64], an = shares[n * 64];
+            const Quarter before_b = fold_read(rows, lane), before_c = fold_read(rows + kFoldRows, lane);
+            float e[kTok], w[kTok], v[kTok];
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) e[t] = dl[t] * a2;
+            __builtin_amdgcn_sched_barrier(0);
+            exp2_burst<kTok>(e);
+            __builtin_amdgcn_sched_barrier(0);
             const State8 s[2] = {s_next[0], s_next[1]};
             const int m = min(n + 1, mine - 1);
+            put_fold(max(n - 1, 0), fold_sum(before_b), fold_sum(before_c));     // (of the first state: of what is there, overwritten by the next)
             a_next = arow[m];
-            h_next = start_of(b, m);
+            h_next = zero ? 0.f : begin[(int64_t)m * a.D];
             s_next[0] = state8(from + m * 2 * kHalf);
             s_next[1] = state8(from + m * 2 * kHalf + half);
-            float e[kTok], w[kTok], v[kTok];
-            arguments<kTok>(dl, a2, dx, [&](int t) { return s[t / kHalf].b(t % kHalf); }, e, v);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) {
                 w[t] = e[t] * h;                                 // a h_{t-1}
-                h = w[t] + v[t];
+                h = fmaf(s[t / kHalf].b(t % kHalf), dx[t], w[t]);
                 out[t] = fmaf(s[t / kHalf].c(t % kHalf), h, out[t]);
                 v[t] = ds[t] * h;
             }
-            const float sum_c = fold16(v, lane);
+            fold_put(rows + kFoldRows, v, lane);
 #pragma unroll
             for (int t = kTok - 1; t >= 0; --t) {
                 gn = fmaf(s[t / kHalf].c(t % kHalf), ds[t], gn);
@@ -295,47 +351,50 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
                 v[t] = gn * dx[t];
                 gn *= e[t];
             }
-            const float sum_b = fold16(v, lane);
-            const float folded = (lane & 1) ? sum_c : sum_b;     // (two lanes each hold the same value for the same place)
-            const int spot = n * 2 * kTok + 2 * (lane >> 2) + (lane & 1);
-            if constexpr (GROUPS == 1) s_fold[wave][spot] = folded;
-            else a.part_bc[place * 2 * kTok + spot] = folded;
+            fold_put(rows, v, lane);
             grads[n * 64] = gn;
-            if (on) part[(int64_t)n * a.D] = an;
+            shares[n * 64] = an;
         }
+        // what only the end needs is read again (from the cache): kept, it would take the registers of a state's work
+        request(b, count);
+        if constexpr (GATED) request_rest(b, count);
+        if (mine > 0) put_fold(mine - 1, fold_sum(fold_read(rows, lane)), fold_sum(fold_read(rows + kFoldRows, lane)));
         if constexpr (GROUPS == 1) {                             // dB and dC of the block, over the workgroup's channels
             __syncthreads();
             for (int i = (int)threadIdx.x; i < a.N * 2 * kTok; i += 64 * WAVES) {
                 float sum = 0.f;
 #pragma unroll
-                for (int k = 0; k < WAVES; ++k) sum += s_fold[k][i];
+                for (int k = 0; k < WAVES; ++k) sum += s_mem[k][kFoldAt + i];
                 a.part_bc[place * 2 * kTok + i] = sum;
             }
             __syncthreads();
         } else {                                                 // the sums over the waves' states; wave 0 finishes
-            __syncthreads();
             if (wave != 0) {
 #pragma unroll
                 for (int t = 0; t < kTok; ++t) {
-                    s_part[wave - 1][t * 64 + lane] = gb[t];
-                    s_part[wave - 1][(kTok + t) * 64 + lane] = gk[t];
-                    s_part[wave - 1][(2 * kTok + t) * 64 + lane] = out[t];
+                    rows[t * 64 + lane] = gb[t];
+                    rows[(kTok + t) * 64 + lane] = gk[t];
+                    rows[(2 * kTok + t) * 64 + lane] = out[t];
                 }
             }
             __syncthreads();
-            if (wave != 0) continue;
-            for (int k = 0; k + 1 < GROUPS; ++k) {
+            if (wave == 0) {
+                for (int k = 1; k < GROUPS; ++k) {
 #pragma unroll
-                for (int t = 0; t < kTok; ++t) {
-                    gb[t] += s_part[k][t * 64 + lane];
-                    gk[t] += s_part[k][(kTok + t) * 64 + lane];
-                    out[t] += s_part[k][(2 * kTok + t) * 64 + lane];
+                    for (int t = 0; t < kTok; ++t) {
+                        gb[t] += s_mem[k][t * 64 + lane];
+                        gk[t] += s_mem[k][(kTok + t) * 64 + lane];
+                        out[t] += s_mem[k][(2 * kTok + t) * 64 + lane];
+                    }
                 }
             }
+            __syncthreads();
+            if (wave != 0) {
+                request(next, next_count);
+                request_rest(next, next_count);
+                continue;
+            }
         }
-        // what only the end needs is read again (from the cache): kept, it would take the registers of a state's work
-        const Tokens<T, kTok> u = load_tokens<T, kTok>(Rows<T>(a.u, a.u_stride, first), count, off),
-                              delta = load_tokens<T, kTok>(Rows<T>(a.delta, a.d_stride, first), count, off);
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
             gk[t] = fmaf(u.at(t), gb[t], gk[t] * kLn2);
@@ -343,11 +402,12 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             dskip = fmaf(ds[t], u.at(t), dskip);                 // (ds is 0 for tokens that are not there)
             out[t] = fmaf(skip, u.at(t), out[t]);
         }
+        float sig[kTok];
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) sig[t] = -(delta.at(t) + bias) * kLog2e;
+        request(next, next_count);
         if (on) store_tokens<T, kTok>(Rows<T>(a.du, a.du_stride, first), count, off, gb);
         if (sp) {                                                // times sigmoid(delta + bias)
-            float sig[kTok];
-#pragma unroll
-            for (int t = 0; t < kTok; ++t) sig[t] = -(delta.at(t) + bias) * kLog2e;
             exp2_burst<kTok>(sig);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) sig[t] += 1.f;
@@ -359,9 +419,6 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
         for (int t = 0; t < kTok; ++t) dbias += t < count ? gk[t] : 0.f;
         if (on) store_tokens<T, kTok>(Rows<T>(a.ddelta, a.dd_stride, first), count, off, gk);
         if constexpr (GATED) {
-            const Tokens<T, kTok> z = load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off),
-                                  dy = load_tokens<T, kTok>(Rows<T>(a.dy, a.dy_stride, first), count, off);
-            float sig[kTok];
 #pragma unroll
             for (int t = 0; t < kTok; ++t) sig[t] = -z.at(t) * kLog2e;
             exp2_burst<kTok>(sig);
@@ -370,10 +427,15 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             rcp_burst<kTok>(sig);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) out[t] *= dy.at(t) * (sig[t] * fmaf(z.at(t), 1.f - sig[t], 1.f));
+            request_rest(next, next_count);
             if (on) store_tokens<T, kTok>(Rows<T>(a.dz, a.dz_stride, first), count, off, out);
+        } else {
+            request_rest(next, next_count);
         }
     }
-    if (!on || n0 != 0) return;
+    if (!on) return;
+    for (int n = 0; n < mine; ++n) part[(int64_t)n * a.D] = shares[n * 64];
+    if (n0 != 0) return;
     part[(int64_t)a.N * a.D] = dskip;
     part[(int64_t)(a.N + 1) * a.D] = dbias;
 }
@@ -423,7 +485,7 @@ __global__ __launch_bounds__(256) void k_packed_bwd_a(PackedScanArgs a)
 
 // The workspace's parts, in floats.
 struct Space {
-    int64_t bc, ends, backs, sums, part_bc, part_a, all;
+    int64_t bc, ends, backs, sums, starts, part_bc, part_a, all;
 };
 Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
 {
@@ -431,10 +493,11 @@ Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
     const int64_t groups = channel_groups(D, N);
     Space s;
     s.bc = 0;
-    s.ends = s.bc + l.max_blocks * N * 32 + 32;                  // (the loop over the states asks for one more than there is)
+    s.ends = s.bc + l.max_blocks * N * 32 + 48;                  // (the loop over the states asks for three more than there are)
     s.backs = s.ends + tiles * N * D;
     s.sums = s.backs + tiles * N * D;
-    s.part_bc = s.sums + tiles * D;
+    s.starts = s.sums + tiles * D;
+    s.part_bc = s.starts + l.max_tiles * (tile / kTok - 1) * N * D;
     s.part_a = s.part_bc + groups * l.max_blocks * 32 * N;
     s.all = s.part_a + l.max_tiles * (N + 2) * D;
     return s;
@@ -492,7 +555,7 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
     a.du = du; a.ddelta = ddelta; a.dz = dz; a.dB = dB; a.dC = dC;
     a.du_stride = du_stride; a.dd_stride = ddelta_stride; a.dz_stride = dz_stride; a.db_stride = dB_stride; a.dc_stride = dC_stride;
     a.dA = dA; a.dD = dDv; a.dbias = ddelta_bias;
-    a.bc = ws + w.bc; a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
+    a.bc = ws + w.bc; a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.starts = ws + w.starts; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
     a.D = (int32_t)D; a.N = (int32_t)N;
     a.softplus = delta_softplus ? 1 : 0;
     a.blocks = (int32_t)l.max_blocks;
@@ -502,24 +565,18 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
     if (l.max_tiles * groups > INT32_MAX || 2 * columns * (l.max_longs + 1) > INT32_MAX || relay > INT32_MAX)
         return fail(COREY_ESHAPE, "%s: T * D is too large", who);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipError_t attr = hipSuccess;
     by_type(dt, [&](auto t) {
         using T = decltype(t);
         by_groups(N, [&](auto gr) {
             constexpr int G = decltype(gr)::value;
             const auto go = [&](auto gate, auto whole) {
                 constexpr bool Z = decltype(gate)::value;
-                const size_t lds = (size_t)Shape<G>::waves * (size_t)kept(pack->tile) * kStates * 64 * 4;
-                // (what the longest tile takes, whatever this call's: another thread's call may be between this line and its launch)
-                constexpr int most = Shape<G>::waves * kept(G == 8 ? 32 : kMaxBackTile) * kStates * 64 * 4;
-                attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_packed_bwd<T, Z, G>), hipFuncAttributeMaxDynamicSharedMemorySize, most);
-                if (attr != hipSuccess) return;
                 k_packed_relay<T><<<(unsigned)relay, 256, 0, stream>>>(a);
                 if (pack->T > pack->tile) {
                     k_packed_bwd_ends<T, Z, G, decltype(whole)::value><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
                     k_packed_bwd_chain<<<(unsigned)(2 * columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
                 }
-                k_packed_bwd<T, Z, G><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, lds, stream>>>(a);
+                k_packed_bwd<T, Z, G><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
             };
             const auto with = [&](auto gate) {
                 if (N == G * kStates) go(gate, std::true_type());
@@ -528,9 +585,8 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
             if (z) with(std::true_type());
             else with(std::false_type());
         });
-        if (attr == hipSuccess) k_packed_bwd_bc<T><<<(unsigned)relay, 256, 0, stream>>>(a);
+        k_packed_bwd_bc<T><<<(unsigned)relay, 256, 0, stream>>>(a);
     });
-    if (attr != hipSuccess) return corey::hip_fail(attr, "corey_scan_packed_bwd: LDS");
     k_packed_bwd_a<<<(unsigned)(((N + 2) * D + 63) / 64), 256, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? corey::hip_fail(e, "corey_scan_packed_bwd launch") : COREY_OK;

@@ -60,12 +60,12 @@ E = {v: k for k, v in binding.STATUS.items()}
 @pytest.mark.parametrize("call, kw, code", [
     (plan, dict(lengths=None), "COREY_ENULL"), (plan, dict(table=None), "COREY_ENULL"), (plan, dict(pack=0), "COREY_ENULL"),
     (plan, dict(S=0), "COREY_ESHAPE"), (plan, dict(S=(1 << 20) + 1), "COREY_ESHAPE"), (plan, dict(T=0), "COREY_ESHAPE"),
-    (plan, dict(T=1 << 31), "COREY_ESHAPE"), (plan, dict(tile=8), "COREY_EINVAL"), (plan, dict(tile=48), "COREY_EINVAL"),
+    (plan, dict(T=1 << 31), "COREY_ESHAPE"), (plan, dict(tile=8), "COREY_EINVAL"), (plan, dict(tile=40), "COREY_EINVAL"),
     (plan, dict(tile=4096), "COREY_EINVAL"), (plan, dict(size=64), "COREY_EWORKSPACE"), (plan, dict(table=ctypes.c_void_p(8200)), "COREY_EWORKSPACE"),
     (conv, dict(x=None), "COREY_ENULL"), (conv, dict(w=None), "COREY_ENULL"), (conv, dict(u=None), "COREY_ENULL"), (conv, dict(u=P), "COREY_EINVAL"),
     (conv, dict(pack=0), "COREY_ENULL"), (conv, dict(pack=index(table=0)), "COREY_ENULL"), (conv, dict(pack=binding.Pack(4096, 100, 0, 1, 64, 0)), "COREY_EINVAL"),
     (conv, dict(pack=index(size=64)), "COREY_EWORKSPACE"), (conv, dict(pack=index(table=4100)), "COREY_EWORKSPACE"),
-    (conv, dict(pack=binding.Pack(4096, 1 << 20, 3, 100, 48, 0)), "COREY_EINVAL"), (conv, dict(dt=7), "COREY_EINVAL"),
+    (conv, dict(pack=binding.Pack(4096, 1 << 20, 3, 100, 40, 0)), "COREY_EINVAL"), (conv, dict(dt=7), "COREY_EINVAL"),
     (conv, dict(W=0), "COREY_EINVAL"), (conv, dict(W=5), "COREY_EINVAL"), (conv, dict(D=0), "COREY_ESHAPE"), (conv, dict(D=(1 << 20) + 1), "COREY_ESHAPE"),
     (conv, dict(xs=7), "COREY_ESHAPE"), (conv, dict(us=0), "COREY_ESHAPE"), (conv, dict(us=1 << 25), "COREY_ESHAPE"),
     (conv, dict(slots=P, state=None), "COREY_ENULL"), (conv, dict(out=P, n_slots=0), "COREY_ENULL"),
@@ -105,7 +105,7 @@ def test_sizes():
     for bad in ((0, 1, 16), (1, 0, 16), (1, 1, 15), (1, 1, 4096), (1 << 21, 1, 16), (1, 1 << 31, 16)):
         assert L.corey_pack_bytes(*bad) == 0
     # B and C as binary32 by blocks of 16 tokens, and the tiles' states where a sequence can have a second tile
-    relaid = lambda T: 4 * ((T // 16 + 3) * 16 * 32 + 32)
+    relaid = lambda T: 4 * ((T // 16 + 3) * 16 * 32 + 48)
     assert L.corey_scan_packed_workspace(ctypes.byref(p), 8, 16) == relaid(100) + 4 * (100 // 64 + 3) * 17 * 8
     assert L.corey_scan_packed_workspace(ctypes.byref(index(T=64)), 8, 16) == relaid(64)
     assert L.corey_scan_packed_workspace(ctypes.byref(p), 8, 129) == 0 and L.corey_scan_packed_bwd_workspace(ctypes.byref(p), 0, 16) == 0
@@ -119,11 +119,12 @@ def test_tile_rule():
             for D in (1, 64, 2048, 5120):
                 for N in (1, 16, 128):
                     tile = t(S, T, D, N)
-                    assert 16 <= tile <= 2048 and tile & (tile - 1) == 0
+                    assert 16 <= tile <= 2048 and tile % 16 == 0
                     back = t(S, T, D, N, backward=True)
-                    assert back in (16, 32, 64) and back <= (32 if N > 64 else 64)
+                    assert back in (16, 32, 48, 64) and back <= (32 if N > 64 else 64)
     assert t(0, 1, 1, 1) == 0 and t(1, 1, 1, 0) == 0
     assert t(1, 1 << 20, 5120) >= t(1, 1 << 14, 5120) >= t(1, 1 << 10, 5120)
+    assert 4096 <= -(-16384 // t(1, 16384, 5120)) * 80 <= 5120   # all tiles run at once
 
 
 def test_parts_of_the_index_are_where_the_header_says():
