@@ -3,10 +3,13 @@
 //     v[t] = bias + sum_k w[k] x[t - (W-1) + k] inside the sequence (before its first token: the slot's state, else 0)
 //     u[t] = v sigmoid(v)
 //
-// Memory bound: 2 values per token and channel forward, 3 backward.  A lane holds V neighbouring channels (16 bytes of them where
-// D allows) and a wave one piece of at most 16 tokens, whose rows it requests all at once, the W-1 rows before it again (they come
-// from the cache, the neighbouring piece is the same workgroup's).
+// Memory bound: 2 values per token and channel forward, 3 backward.  A lane holds V neighbouring channels (four where D allows) and a
+// wave a piece of at most 16 tokens, whose rows it requests eight together; the W-1 rows before the piece come from the cache (the
+// neighbouring piece is the same workgroup's).  16384 tokens of 5120 bf16 channels (337 MB), us: one piece a wave 74, runs of 2, 4, 8, 16
+// pieces, which keep the taps, 78, 83, 83, 101; eight channels a lane as long as four.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "corey_packed.h"
 #include "corey_scan_impl.h"
@@ -32,10 +35,15 @@ template <typename T, int V> __device__ __forceinline__ Vec<T, V> load(const T* 
 }
 template <typename T, int V> __device__ __forceinline__ void store(T* p, const float (&f)[V])
 {
-    Vec<T, V> r;
+    if constexpr (sizeof(T) == 2) {                              // rounded two at a time
+        constexpr int P = (V + 1) / 2;
+        uint32_t w[P];
 #pragma unroll
-    for (int i = 0; i < V; ++i) Io<T>::st(&r.v[i], f[i]);
-    __builtin_memcpy(p, &r, sizeof(r));
+        for (int i = 0; i < P; ++i) w[i] = Io<T>::pack2(f[2 * i], f[2 * i + 1 < V ? 2 * i + 1 : 2 * i]);
+        __builtin_memcpy(p, w, V * sizeof(T));
+    } else {
+        __builtin_memcpy(p, f, sizeof(f));
+    }
 }
 
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(-v * kLog2e)); }
@@ -56,6 +64,18 @@ struct ConvArgs {
     int32_t run, runs;
 };
 
+template <typename T, int V, int W> __device__ __forceinline__ void load_taps(const ConvArgs& a, int d, float (&w)[W][V], float (&b)[V])
+{
+    float rows[V][W];                           // [D, W]: a lane's channels are one stretch
+    __builtin_memcpy(rows, a.weight + (int64_t)d * W, sizeof(rows));
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        b[i] = a.bias ? a.bias[d + i] : 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[k][i] = rows[i][k];
+    }
+}
+
 template <typename T, int V, int W>
 __global__ __launch_bounds__(kThreads) void k_conv_packed(ConvArgs a)
 {
@@ -68,35 +88,12 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed(ConvArgs a)
     if (d >= a.D) return;
     constexpr int H = W - 1;
     const T* x = static_cast<const T*>(a.x) + d;
+    T* u = static_cast<T*>(a.u) + d;
     const int64_t xs = a.x_stride;
     float w[W][V], b[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        b[i] = a.bias ? a.bias[d + i] : 0.f;
-#pragma unroll
-        for (int k = 0; k < W; ++k) w[k][i] = a.weight[(int64_t)(d + i) * W + k];
-    }
-    float past[H > 0 ? H : 1][V] = {};          // the inputs before the piece, oldest first
+    load_taps<T, V, W>(a, d, w, b);
+    float past[H > 0 ? H : 1][V] = {};          // the inputs before the next token, oldest first
     const bool first = (p.bits & 1) != 0;
-    const int64_t from = first ? slot_of(a.slots, p.seq, a.n_slots) : -1;
-    T old[V][H > 0 ? H : 1] = {};
-    if constexpr (H > 0) {
-        if (!first) {                           // (pieces before the last have 16 tokens: all of these are the sequence's)
-#pragma unroll
-            for (int j = 0; j < H; ++j) {
-                const Vec<T, V> r = load<T, V>(x + (p.first - H + j) * xs);
-#pragma unroll
-                for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&r.v[i]);
-            }
-        } else if (from >= 0) {
-            __builtin_memcpy(old, static_cast<const T*>(a.state) + (from * a.D + d) * H, sizeof(old));
-#pragma unroll
-            for (int j = 0; j < H; ++j)
-#pragma unroll
-                for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&old[i][j]);
-        }
-    }
-    T* u = static_cast<T*>(a.u) + d;
     // groups of tokens: the rows of a group are requested together
     auto tokens = [&](int t0, auto count) {
         constexpr int C = decltype(count)::value;
@@ -124,8 +121,27 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed(ConvArgs a)
             }
         }
     };
+    T old[V][H > 0 ? H : 1] = {};
+    if constexpr (H > 0) {
+        if (first) {
+            const int64_t from = slot_of(a.slots, p.seq, a.n_slots);
+            if (from >= 0) __builtin_memcpy(old, static_cast<const T*>(a.state) + (from * a.D + d) * H, sizeof(old));
+#pragma unroll
+            for (int j = 0; j < H; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&old[i][j]);
+        } else {                                // (pieces before the last have 16 tokens: all of these are the sequence's)
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                const Vec<T, V> r = load<T, V>(x + (int64_t)(p.first - H + j) * xs);
+#pragma unroll
+                for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&r.v[i]);
+            }
+        }
+    }
     if (p.count == kBlock) {
-        tokens(0, std::integral_constant<int, kBlock>());
+#pragma unroll 1
+        for (int t = 0; t < kBlock; t += kBlock / 2) tokens(t, std::integral_constant<int, kBlock / 2>());
     } else {
         int t = 0;
         for (; t + 4 <= p.count; t += 4) tokens(t, std::integral_constant<int, 4>());
@@ -134,14 +150,13 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed(ConvArgs a)
     // The state moves on: the last W-1 of (old state, inputs).  The wave that has read the old state writes the new one, so a
     // slot that is read and written by one sequence is in no race.
     if constexpr (H > 0) {
-        if (!first) return;
-        const int64_t to = slot_of(a.slots_out, p.seq, a.n_slots);
+        const int64_t to = first ? slot_of(a.slots_out, p.seq, a.n_slots) : -1;
         if (to < 0) return;
         const int begin = p.first, len = a.ix.starts[p.seq + 1] - begin;
         T now[V][H];
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-            const int t = len - H + j;          // before the first token: the old state's
+            const int t = len - H + j;      // before the first token: the old state's
             if (t >= 0) {
                 const Vec<T, V> r = load<T, V>(x + (int64_t)(begin + t) * xs);
 #pragma unroll
@@ -160,8 +175,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed(ConvArgs a)
 }
 
 // Gradients.  With dv[t] = du[t] silu'(v[t]):  dx[t] = sum_k w[k] dv[t + (W-1) - k] (0 behind the sequence's end),
-// dw[k] = sum_t dv[t] x[t - (W-1) + k], dbias = sum_t dv[t].  v is formed again.  A wave walks a run of pieces and keeps its sums
-// of dw and dbias in registers; a second kernel adds up the runs, always in the same order.
+// dw[k] = sum_t dv[t] x[t - (W-1) + k], dbias = sum_t dv[t].  v is formed again.  A wave walks a run of pieces and keeps the last W
+// dv and its sums of dw and dbias in registers; dx lies W-1 tokens behind, and where the run ends inside a sequence the next W-1
+// tokens are looked at for it.  A second kernel adds up the runs, always in the same order.
 template <typename T, int V, int W>
 __global__ __launch_bounds__(kThreads) void k_conv_packed_bwd(ConvArgs a)
 {
@@ -175,78 +191,97 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed_bwd(ConvArgs a)
     const T* du = static_cast<const T*>(a.du) + d;
     T* dx = static_cast<T*>(a.dx) + d;
     float w[W][V], b[V], dw[W][V] = {}, db[V] = {};
+    load_taps<T, V, W>(a, d, w, b);
+    float past[H > 0 ? H : 1][V] = {}, dv[W][V] = {};            // the inputs before the next token; dv of the last W, oldest first
+    int behind = 0;                             // tokens (at most W-1) whose dx is still to come
+    // dv of one more token joins, and the dx that it completes (of the token W-1 rows before `row`) is stored
+    const auto join = [&](int64_t row, const float (&g)[V]) {
+        float out[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        b[i] = a.bias ? a.bias[d + i] : 0.f;
+        for (int i = 0; i < V; ++i) {
 #pragma unroll
-        for (int k = 0; k < W; ++k) w[k][i] = a.weight[(int64_t)(d + i) * W + k];
-    }
-    const int64_t stop = min((int64_t)a.pieces, (run + 1) * a.run);
-    for (int64_t at = run * a.run; at < stop; ++at) {
-        const Piece p = a.ix.blocks[at];
-        if (p.seq < 0) break;                   // the used pieces come first
-        const int end = a.ix.starts[p.seq + 1];
-        const int ahead = min(H, end - (p.first + p.count));       // tokens behind the piece whose dv its dx needs
-        float past[H > 0 ? H : 1][V] = {}, dv[W][V] = {};           // dv: of the last W tokens, oldest first
-        if constexpr (H > 0) {
-            if (!(p.bits & 1)) {
+            for (int k = 0; k < H; ++k) dv[k][i] = dv[k + 1][i];
+            dv[H][i] = g[i];
+            float sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < H; ++j) {
-                    const Vec<T, V> r = load<T, V>(x + (p.first - H + j) * a.x_stride);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&r.v[i]);
-                }
-            }
+            for (int k = 0; k < W; ++k) sum = fmaf(w[k][i], dv[H - k][i], sum);
+            out[i] = sum;
         }
-        // token e of the piece (or behind it); dx of token e - H is ready then
-        auto token = [&](int e, const Vec<T, V>& rx, const Vec<T, V>& rg, bool real, bool mine) {
-            float out[V];
+        if (behind == H) store<T, V>(dx + (row - H) * a.dx_stride, out);
+        else ++behind;
+    };
+    const auto tokens = [&](int64_t row, auto count, auto mine) {      // (mine: they count for dw and dbias)
+        constexpr int C = decltype(count)::value;
+        Vec<T, V> rx[C], rg[C];
+#pragma unroll
+        for (int t = 0; t < C; ++t) {
+            rx[t] = load<T, V>(x + (row + t) * a.x_stride);
+            rg[t] = load<T, V>(du + (row + t) * a.du_stride);
+        }
+#pragma unroll
+        for (int t = 0; t < C; ++t) {
+            float g[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float now = Io<T>::ld(&rx.v[i]);
+                const float now = Io<T>::ld(&rx[t].v[i]);
                 float s = b[i];
 #pragma unroll
                 for (int k = 0; k < H; ++k) s = fmaf(w[k][i], past[k][i], s);
                 s = fmaf(w[H][i], now, s);
                 const float sig = sigmoid(s);
-                const float g = real ? Io<T>::ld(&rg.v[i]) * (sig * fmaf(s, 1.f - sig, 1.f)) : 0.f;
+                g[i] = Io<T>::ld(&rg[t].v[i]) * (sig * fmaf(s, 1.f - sig, 1.f));
+                if constexpr (decltype(mine)::value) {
 #pragma unroll
-                for (int k = 0; k < H; ++k) dv[k][i] = dv[k + 1][i];
-                dv[H][i] = g;
-                const float own = mine ? g : 0.f;
-#pragma unroll
-                for (int k = 0; k < H; ++k) dw[k][i] = fmaf(own, past[k][i], dw[k][i]);
-                dw[H][i] = fmaf(own, now, dw[H][i]);
-                db[i] += own;
-                float sum = 0.f;
-#pragma unroll
-                for (int k = 0; k < W; ++k) sum = fmaf(w[k][i], dv[H - k][i], sum);
-                out[i] = sum;
+                    for (int k = 0; k < H; ++k) dw[k][i] = fmaf(g[i], past[k][i], dw[k][i]);
+                    dw[H][i] = fmaf(g[i], now, dw[H][i]);
+                    db[i] += g[i];
+                }
 #pragma unroll
                 for (int k = 0; k + 1 < H; ++k) past[k][i] = past[k + 1][i];
                 if constexpr (H > 0) past[H - 1][i] = now;
             }
-            if (e >= H) store<T, V>(dx + (int64_t)(p.first + e - H) * a.dx_stride, out);
-        };
-        auto tokens = [&](int e0, auto count) {
-            constexpr int C = decltype(count)::value;
-            Vec<T, V> rx[C], rg[C];
+            join(row + t, g);
+        }
+    };
+    using One = std::integral_constant<int, 1>;
+    const int64_t stop = min((int64_t)a.pieces, (run + 1) * a.run);
+    for (int64_t at = run * a.run; at < stop; ++at) {
+        const Piece p = a.ix.blocks[at];
+        if (p.seq < 0) break;                   // the used pieces come first
+        if ((p.bits & 1) || at == run * a.run) {
+            behind = 0;
 #pragma unroll
-            for (int t = 0; t < C; ++t) {       // rows behind the sequence are replaced by its last
-                const int64_t row = min((int64_t)p.first + e0 + t, (int64_t)end - 1);
-                rx[t] = load<T, V>(x + row * a.x_stride);
-                rg[t] = load<T, V>(du + row * a.du_stride);
-            }
+            for (int j = 0; j < H; ++j) {
+                if (p.bits & 1) {
 #pragma unroll
-            for (int t = 0; t < C; ++t) {
-                const int e = e0 + t;
-                token(e, rx[t], rg[t], e < p.count + ahead, e < p.count);
+                    for (int i = 0; i < V; ++i) past[j][i] = 0.f;
+                } else {
+                    const Vec<T, V> r = load<T, V>(x + (int64_t)(p.first - H + j) * a.x_stride);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) past[j][i] = Io<T>::ld(&r.v[i]);
+                }
             }
-        };
+        }
         if (p.count == kBlock) {
-            tokens(0, std::integral_constant<int, kBlock + H>());
+#pragma unroll 1
+            for (int t = 0; t < kBlock; t += kBlock / 2) tokens((int64_t)p.first + t, std::integral_constant<int, kBlock / 2>(), std::true_type());
         } else {
-            for (int e = 0; e < p.count + H; ++e) tokens(e, std::integral_constant<int, 1>());
+            for (int t = 0; t < p.count; ++t) tokens((int64_t)p.first + t, One(), std::true_type());
+        }
+        if constexpr (H > 0) {
+            if (!(p.bits & 2) && at + 1 < stop) continue;
+            // the sequence or the run ends: what follows completes the dx still to come (nothing follows a sequence)
+            const int64_t row = (int64_t)p.first + p.count;
+            const int follow = (int)min((int64_t)H, (int64_t)a.ix.starts[p.seq + 1] - row);
+            const float none[V] = {};
+            const int due = behind;
+            // (a sequence shorter than W-1: its first dx is complete only when as many have joined)
+            for (int j = 0, left = due; left > 0; ++j) {
+                const bool out = behind == H;
+                if (j < follow) tokens(row + j, One(), std::false_type());
+                else join(row + j, none);
+                left -= out ? 1 : 0;
+            }
         }
     }
 #pragma unroll
@@ -256,25 +291,27 @@ __global__ __launch_bounds__(kThreads) void k_conv_packed_bwd(ConvArgs a)
 }
 
 // Sums over the runs, [runs, W + 1, D] -> dweight [D, W] and dbias [D].  A workgroup takes 64 columns; its waves the runs in turn.
-__global__ __launch_bounds__(kThreads) void k_conv_packed_sum(ConvArgs a, int W, float* dweight, float* dbias)
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(64 * kSumWaves) void k_conv_packed_sum(ConvArgs a, int W, float* dweight, float* dbias)
 {
-    __shared__ float part[kWaves][64];
+    __shared__ float part[kSumWaves][64];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const int64_t n = (int64_t)(W + 1) * a.D, col = (int64_t)blockIdx.x * 64 + lane;
     float s[4] = {};
     if (col < n && a.ix.good()) {
         int r = wave;
-        for (; r + 3 * kWaves < a.runs; r += 4 * kWaves) {
+        for (; r + 3 * kSumWaves < a.runs; r += 4 * kSumWaves) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] += a.parts[(r + q * kWaves) * n + col];
+            for (int q = 0; q < 4; ++q) s[q] += a.parts[(r + q * kSumWaves) * n + col];
         }
-        for (; r < a.runs; r += kWaves) s[0] += a.parts[r * n + col];
+        for (; r < a.runs; r += kSumWaves) s[0] += a.parts[r * n + col];
     }
     part[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
     if (wave != 0 || col >= n) return;
     float sum = 0.f;
-    for (int w = 0; w < kWaves; ++w) sum += part[w][lane];
+#pragma unroll
+    for (int w = 0; w < kSumWaves; ++w) sum += part[w][lane];
     const int k = (int)(col / a.D), d = (int)(col % a.D);
     if (k < W) dweight[(int64_t)d * W + k] = sum;
     else if (dbias) dbias[d] = sum;
@@ -300,10 +337,11 @@ template <typename F> void by_taps(int W, F&& f)
     else f(std::integral_constant<int, 4>());
 }
 
-// Runs of pieces the backward pass is cut into: about 2048 waves fill the GPU, and more runs are more partial sums to add up.
+// Runs of pieces the backward pass is cut into: as many waves as the GPU runs at once (three a SIMD by their registers).  16384 tokens
+// of 5120 bf16 channels, us: 1024 waves 177, 2048 129, 3072 120, 4096 136, 8192 128.
 int64_t runs_of(int64_t pieces, int64_t groups, int32_t* run)
 {
-    const int64_t want = (2048 + groups - 1) / groups;
+    const int64_t want = std::max<int64_t>(1, 3072 / groups);
     *run = (int32_t)((pieces + want - 1) / want);
     return (pieces + *run - 1) / *run;
 }
@@ -350,7 +388,7 @@ extern "C" int corey_conv_packed(const void* x, int64_t x_stride, const float* w
     bool fits = true;
     by_type(dt, [&](auto t) {
         using T = decltype(t);
-        by_width<16 / (int)sizeof(T)>(D, [&](auto v) {
+        by_width<4>(D, [&](auto v) {
             constexpr int V = decltype(v)::value;
             a.groups = (int32_t)((D + 64 * V - 1) / (64 * V));
             const int64_t grid = (l.max_blocks + kWaves - 1) / kWaves * a.groups;
@@ -419,7 +457,7 @@ extern "C" int corey_conv_packed_bwd(const void* x, int64_t x_stride, const floa
             k_conv_packed_bwd<decltype(t), decltype(v)::value, decltype(w)::value><<<grid, kThreads, 0, stream>>>(a);
         });
     });
-    k_conv_packed_sum<<<(unsigned)(((W + 1) * D + 63) / 64), kThreads, 0, stream>>>(a, W, dweight, dbias);
+    k_conv_packed_sum<<<(unsigned)(((W + 1) * D + 63) / 64), 64 * kSumWaves, 0, stream>>>(a, W, dweight, dbias);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? corey::hip_fail(e, "corey_conv_packed_bwd launch") : COREY_OK;
 }
