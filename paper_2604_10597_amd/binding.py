@@ -57,30 +57,21 @@ class Pack(ctypes.Structure):
     _fields_ = [("_table", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("S", ctypes.c_int64), ("T", ctypes.c_int64),
                 ("tile", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
-    def _at(self, part: int) -> int:
-        """The word a part begins at: starts, seq, tiles, blocks (include/corey.h)."""
-        up = lambda n: -(-n // 4) * 4
-        sizes = (16, up(self.S + 1), up(self.T), 4 * self._pieces(self.tile))
-        return sum(sizes[:part + 1])
-
-    def _pieces(self, size: int) -> int:
-        return self.T // size + min(self.S, self.T)
-
     @property
     def starts(self) -> torch.Tensor:
-        return self.table.as_strided((self.S + 1,), (1,), self.table.storage_offset() + self._at(0))
+        return (_ext or _native()).pack_part(self, 0)
 
     @property
     def seq(self) -> torch.Tensor:
-        return self.table.as_strided((self.T,), (1,), self.table.storage_offset() + self._at(1))
+        return (_ext or _native()).pack_part(self, 1)
 
     @property
     def tiles(self) -> torch.Tensor:
-        return self.table.as_strided((self._pieces(self.tile), 4), (4, 1), self.table.storage_offset() + self._at(2))
+        return (_ext or _native()).pack_part(self, 2)
 
     @property
     def blocks(self) -> torch.Tensor:
-        return self.table.as_strided((self._pieces(16), 4), (4, 1), self.table.storage_offset() + self._at(3))
+        return (_ext or _native()).pack_part(self, 3)
 
 
 _lib = None

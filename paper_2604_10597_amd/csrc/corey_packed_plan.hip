@@ -37,24 +37,38 @@ __device__ __forceinline__ uint32_t add_capped(uint32_t a, uint32_t b, uint32_t 
     return s < cap ? s : cap;
 }
 
-// Inclusive capped sums over the workgroup's lanes; `scratch` has a word per wave.
-__device__ uint32_t scan_lanes(uint32_t v, uint32_t cap, uint32_t* scratch, uint32_t* total)
+// Exclusive sums of several counts over the workgroup's lanes, each capped, and the sums of all; `scratch` has a word per wave and count.
+template <int C> __device__ void scan_lanes(uint32_t (&v)[C], const uint32_t (&cap)[C], uint32_t (*scratch)[kWavesPer], uint32_t (&all)[C])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t up[C];
+#pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(v, d);
-        if (lane >= d) v = add_capped(v, o, cap);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const uint32_t o = __shfl_up(v[c], d);
+            if (lane >= d) v[c] = add_capped(v[c], o, cap[c]);
+        }
     }
-    if (lane == 63) scratch[wave] = v;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-    for (int w = 0; w < kWavesPer; ++w) {
-        if (w == wave) before = all;
-        all = add_capped(all, scratch[w], cap);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (lane == 63) scratch[c][wave] = v[c];
+        up[c] = __shfl_up(v[c], 1);
+        if (lane == 0) up[c] = 0;
     }
     __syncthreads();
-    *total = all;
-    return add_capped(before, v, cap);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        uint32_t before = 0;
+        all[c] = 0;
+#pragma unroll
+        for (int w = 0; w < kWavesPer; ++w) {
+            if (w == wave) before = all[c];
+            all[c] = add_capped(all[c], scratch[c][w], cap[c]);
+        }
+        v[c] = add_capped(before, up[c], cap[c]);
+    }
+    __syncthreads();
 }
 
 struct Sums {
@@ -65,43 +79,37 @@ struct Sums {
 // the list of the sequences of more than one tile (where `longs` is given; s0: the first one's number).  A lane takes kRun sequences
 // in a row, all of their lengths in one trip to memory.  Returns the sums behind the last.
 __device__ Sums sum_up(const PlanArgs& a, int s0, int n, Sums before, int32_t* starts, int32_t* tile_begin, int32_t* block_begin,
-                       int32_t* longs, uint32_t* scratch)
+                       int32_t* longs, uint32_t (*scratch)[kWavesPer])
 {
-    const uint32_t cap = (uint32_t)a.T, no_cap = 0x7fffffffu;
+    const uint32_t cap = (uint32_t)a.T;
     const int first = (int)threadIdx.x * kRun;
     const int32_t* lengths = a.lengths + s0;
-    uint32_t len[kRun], sum = 0, all;
+    uint32_t len[kRun], sum[1] = {}, all[1];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) len[i] = first + i < n ? (uint32_t)min(max(lengths[first + i], 0), a.T) : 0u;
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) sum = add_capped(sum, len[i], cap);
-    // the lanes before this one end where it begins
-    const uint32_t end = scan_lanes(sum, cap, scratch, &all);
-    uint32_t at = __shfl_up(end, 1);
-    if ((threadIdx.x & 63) == 63) scratch[threadIdx.x >> 6] = end;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) at = threadIdx.x == 0 ? 0u : scratch[(threadIdx.x >> 6) - 1];
-    __syncthreads();
-    at = add_capped(before.tokens, at, cap);
-    uint32_t nt = 0, nb = 0, nl = 0;
+    for (int i = 0; i < kRun; ++i) sum[0] = add_capped(sum[0], len[i], cap);
+    scan_lanes<1>(sum, {cap}, scratch, all);
+    uint32_t at = add_capped(before.tokens, sum[0], cap);
+    uint32_t pieces[3] = {}, of_all[3];                         // tiles, blocks, sequences of more than one tile
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         const uint32_t next = add_capped(at, len[i], cap);
         if (first + i < n) starts[first + i] = (int32_t)at;
         len[i] = next - at;                                     // what of it fits
-        nt += (len[i] + a.tile - 1) / (uint32_t)a.tile;
-        nb += (len[i] + kBlock - 1) / kBlock;
-        nl += len[i] > (uint32_t)a.tile;
+        pieces[0] += (len[i] + a.tile - 1) / (uint32_t)a.tile;
+        pieces[1] += (len[i] + kBlock - 1) / kBlock;
+        pieces[2] += len[i] > (uint32_t)a.tile;
         at = next;
     }
+    const uint32_t none = 0x7fffffffu;
+    scan_lanes<3>(pieces, {none, none, none}, scratch, of_all);
     Sums out;
-    out.tokens = add_capped(before.tokens, all, cap);
-    uint32_t tb = before.tiles + scan_lanes(nt, no_cap, scratch, &all) - nt;
-    out.tiles = before.tiles + all;
-    uint32_t bb = before.blocks + scan_lanes(nb, no_cap, scratch, &all) - nb;
-    out.blocks = before.blocks + all;
-    uint32_t lb = before.longs + scan_lanes(nl, no_cap, scratch, &all) - nl;
-    out.longs = before.longs + all;
+    out.tokens = add_capped(before.tokens, all[0], cap);
+    out.tiles = before.tiles + of_all[0];
+    out.blocks = before.blocks + of_all[1];
+    out.longs = before.longs + of_all[2];
+    uint32_t tb = before.tiles + pieces[0], bb = before.blocks + pieces[1], lb = before.longs + pieces[2];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         if (first + i < n) {
@@ -196,7 +204,7 @@ __device__ void write_head(const PlanArgs& a, const Sums& all)
 __global__ __launch_bounds__(kThreads) void k_pack_small(PlanArgs a)
 {
     __shared__ int32_t s_starts[kOneLaunch + 1], s_tiles[kOneLaunch + 1], s_blocks[kOneLaunch + 1];
-    __shared__ uint32_t scratch[kWavesPer];
+    __shared__ uint32_t scratch[3][kWavesPer];
     const Sums all = sum_up(a, 0, a.S, Sums{0, 0, 0, 0}, s_starts, s_tiles, s_blocks, blockIdx.x == 0 ? a.longs : nullptr, scratch);
     if (blockIdx.x == 0) {
         for (int s = threadIdx.x; s <= a.S; s += kThreads) {
@@ -211,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void k_pack_small(PlanArgs a)
 
 __global__ __launch_bounds__(kThreads) void k_pack_sums(PlanArgs a)
 {
-    __shared__ uint32_t scratch[kWavesPer];
+    __shared__ uint32_t scratch[3][kWavesPer];
     Sums at{0, 0, 0, 0};
     for (int s = 0; s < a.S; s += kOneLaunch)                   // (the next part overwrites this one's end with the same value)
         at = sum_up(a, s, min(kOneLaunch, a.S - s), at, a.starts + s, a.tile_begin + s, a.block_begin + s, a.longs, scratch);

@@ -854,6 +854,24 @@ PyObject* pack_plan(PyObject* const* a)      // lengths, T, tile, table, pack
     return wrap(table);
 }
 
+// A part of the index as a view of the table: 0 starts, 1 seq, 2 tiles, 3 blocks (include/corey.h says where they lie).
+PyObject* pack_part(PyObject* const* a)      // pack, part
+{
+    const corey_pack* p = structure<corey_pack>(a[0], "pack");
+    const int64_t part = integer(a[1]);
+    const Owned o(PyObject_GetAttrString(a[0], "table"));
+    if (!o.o) throw PyError{};
+    const at::Tensor& t = tensor(o.o, "pack.table");
+    const auto up = [](int64_t n) { return (n + 3) / 4 * 4; };
+    const auto pieces = [&](int64_t size) { return p->T / size + (p->S < p->T ? p->S : p->T); };
+    if (p->tile < 1 || t.data_ptr() != p->table || t.nbytes() < p->bytes) raise(PyExc_ValueError, "pack is not as corey_pack_plan left it");
+    const int64_t starts = 16, seq = starts + up(p->S + 1), tiles = seq + up(p->T), blocks = tiles + 4 * pieces(p->tile), from = t.storage_offset();
+    if (part == 0) return wrap(t.as_strided({p->S + 1}, {1}, from + starts));
+    if (part == 1) return wrap(t.as_strided({p->T}, {1}, from + seq));
+    if (part == 2) return wrap(t.as_strided({pieces(p->tile), 4}, {4, 1}, from + tiles));
+    return wrap(t.as_strided({pieces(COREY_PACK_BLOCK), 4}, {4, 1}, from + blocks));
+}
+
 PyObject* conv_packed(PyObject* const* a)      // x, weight, bias, pack, state, slots, slots_out, u
 {
     const at::Tensor& xt = rows_tensor(a[0], "x");
@@ -1104,6 +1122,7 @@ PyMethodDef methods[] = {
     COREY_ENTRY("corey_select_chunk_device", select_chunk_device, 5),
     COREY_ENTRY("selective_scan_fwd", scan, 19),
     COREY_ENTRY("corey_pack_plan", pack_plan, 5),
+    COREY_ENTRY("pack_part", pack_part, 2),
     COREY_ENTRY("corey_conv_packed", conv_packed, 8),
     COREY_ENTRY("corey_conv_packed_bwd", conv_packed_bwd, 6),
     COREY_ENTRY("corey_scan_packed", scan_packed, 15),

@@ -5,6 +5,7 @@ import os
 
 import numpy as np
 import pytest
+import torch
 
 import packed_ref as ref
 from conftest import ROOT
@@ -128,16 +129,15 @@ def test_tile_rule():
 
 
 def test_parts_of_the_index_are_where_the_header_says():
-    class Table:                                                  # the offsets alone
-        def storage_offset(self):
-            return 5
-
-        def as_strided(self, size, stride, at):
-            return size, stride, at - 5
     p = index(S=6, T=50, tile=16)
-    p.table = Table()
-    assert p.starts == ((7,), (1,), 16) and p.seq == ((50,), (1,), 24)
-    assert p.tiles == ((50 // 16 + 6, 4), (4, 1), 76) and p.blocks == ((50 // 16 + 6, 4), (4, 1), 76 + 36)
+    table = torch.arange(p.bytes // 4 + 5, dtype=torch.int32)[5:]
+    p.table, p._table = table, table.data_ptr()
+    at = lambda part: (tuple(part.shape), part.stride(), (part.data_ptr() - table.data_ptr()) // 4)
+    assert at(p.starts) == ((7,), (1,), 16) and at(p.seq) == ((50,), (1,), 24)
+    assert at(p.tiles) == ((50 // 16 + 6, 4), (4, 1), 76) and at(p.blocks) == ((50 // 16 + 6, 4), (4, 1), 76 + 36)
+    p.table = table[1:]                                           # another table than the index was built in
+    with pytest.raises(ValueError):
+        p.starts
 
 
 # ------------------------------------------------------------------------------------------- the reference
