@@ -94,6 +94,9 @@ __device__ __forceinline__ int64_t slot_of(const int32_t* slots, int seq, int64_
 constexpr int64_t kMaxStride = (int64_t)1 << 25;
 inline bool good_stride(int64_t stride, int64_t D) { return stride >= D && stride < kMaxStride; }
 
+// A launch has fewer than 2^32 lanes.
+inline bool good_grid(int64_t groups, int64_t threads) { return groups * threads <= UINT32_MAX; }
+
 inline bool good_dtype(corey_dtype dt) { return dt == COREY_F32 || dt == COREY_BF16 || dt == COREY_F16; }
 
 // f(T()) with the storage type of dt.

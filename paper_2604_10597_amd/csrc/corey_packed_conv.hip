@@ -308,7 +308,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_conv_packed_sum(ConvArgs a, 
     }
     part[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
-    if (wave != 0 || col >= n) return;
+    if (wave != 0 || col >= n || !a.ix.good()) return;
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kSumWaves; ++w) sum += part[w][lane];
@@ -317,17 +317,18 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_conv_packed_sum(ConvArgs a, 
     else if (dbias) dbias[d] = sum;
 }
 
-// The widest vector of channels, at most `most`, that D is whole numbers of (a lane's channels are all there or none is).
-template <int MOST, typename F> void by_width(int64_t D, F&& f)
+// Channels of a lane: four, or as many as D is whole numbers of (a lane's channels are all there or none is).
+template <typename F> void by_width(int64_t D, F&& f)
 {
-    if constexpr (MOST >= 8) {
-        if (D % 8 == 0) return f(std::integral_constant<int, 8>());
-    }
-    if constexpr (MOST >= 4) {
-        if (D % 4 == 0) return f(std::integral_constant<int, 4>());
-    }
+    if (D % 4 == 0) return f(std::integral_constant<int, 4>());
     if (D % 2 == 0) return f(std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 1>());
+}
+int64_t groups_of(int64_t D)                    // of 64 lanes' channels
+{
+    int64_t wide = 0;
+    by_width(D, [&](auto v) { wide = 64 * decltype(v)::value; });
+    return (D + wide - 1) / wide;
 }
 template <typename F> void by_taps(int W, F&& f)
 {
@@ -337,11 +338,12 @@ template <typename F> void by_taps(int W, F&& f)
     else f(std::integral_constant<int, 4>());
 }
 
-// Runs of pieces the backward pass is cut into: as many waves as the GPU runs at once (three a SIMD by their registers).  16384 tokens
-// of 5120 bf16 channels, us: 1024 waves 177, 2048 129, 3072 120, 4096 136, 8192 128.
+// Runs of pieces the backward pass is cut into: as many waves as the GPU runs at once, three a SIMD by their registers.  16384 tokens of
+// 5120 bf16 channels, us: one wave a SIMD 177, two 129, three 120, four 136, eight 128.
+constexpr int64_t kWavesAtOnce = 3 * 4 * 256;
 int64_t runs_of(int64_t pieces, int64_t groups, int32_t* run)
 {
-    const int64_t want = std::max<int64_t>(1, 3072 / groups);
+    const int64_t want = std::max<int64_t>(1, kWavesAtOnce / groups);
     *run = (int32_t)((pieces + want - 1) / want);
     return (pieces + *run - 1) / *run;
 }
@@ -388,11 +390,11 @@ extern "C" int corey_conv_packed(const void* x, int64_t x_stride, const float* w
     bool fits = true;
     by_type(dt, [&](auto t) {
         using T = decltype(t);
-        by_width<4>(D, [&](auto v) {
+        by_width(D, [&](auto v) {
             constexpr int V = decltype(v)::value;
-            a.groups = (int32_t)((D + 64 * V - 1) / (64 * V));
+            a.groups = (int32_t)groups_of(D);
             const int64_t grid = (l.max_blocks + kWaves - 1) / kWaves * a.groups;
-            fits = grid <= INT32_MAX;
+            fits = good_grid(grid, kThreads);
             if (!fits) return;
             by_taps(W, [&](auto w) { k_conv_packed<T, V, decltype(w)::value><<<(unsigned)grid, kThreads, 0, stream>>>(a); });
         });
@@ -402,23 +404,12 @@ extern "C" int corey_conv_packed(const void* x, int64_t x_stride, const float* w
     return e != hipSuccess ? corey::hip_fail(e, "corey_conv_packed launch") : COREY_OK;
 }
 
-namespace {
-// Channels of a lane in the backward pass: 8 bytes of 16-bit values, 16 of binary32 (its window of rows takes the registers).
-template <typename F> void by_backward_width(corey_dtype dt, int64_t D, F&& f)
-{
-    by_type(dt, [&](auto t) { by_width<4>(D, [&](auto v) { f(t, v); }); });
-}
-int64_t backward_width(int64_t D) { return D % 4 == 0 ? 4 : D % 2 == 0 ? 2 : 1; }
-}  // namespace
-
 extern "C" size_t corey_conv_packed_bwd_workspace(const corey_pack* pack, int64_t D, int32_t W)
 {
     Index ix;
     if (W < 1 || W > COREY_MAX_CONV || D < 1 || D > COREY_PACK_MAX_CHANNELS || index_of("corey_conv_packed_bwd_workspace", pack, &ix)) return 0;
-    const Layout l = layout(pack->S, pack->T, pack->tile);
-    const int64_t wide = 64 * backward_width(D);
     int32_t run;
-    return (size_t)(runs_of(l.max_blocks, (D + wide - 1) / wide, &run) * (W + 1) * D) * 4;
+    return (size_t)(runs_of(layout(pack->S, pack->T, pack->tile).max_blocks, groups_of(D), &run) * (W + 1) * D) * 4;
 }
 
 extern "C" int corey_conv_packed_bwd(const void* x, int64_t x_stride, const float* weight, const float* bias, const void* du,
@@ -436,7 +427,6 @@ extern "C" int corey_conv_packed_bwd(const void* x, int64_t x_stride, const floa
     if (!workspace || workspace_bytes < corey_conv_packed_bwd_workspace(pack, D, W) || reinterpret_cast<uintptr_t>(workspace) % 4 != 0)
         return fail(COREY_EWORKSPACE, "%s: workspace missing, misaligned or smaller than corey_conv_packed_bwd_workspace()", who);
     const Layout l = layout(pack->S, pack->T, pack->tile);
-    const int64_t wide = 64 * backward_width(D);
     a.x = x;
     a.weight = weight;
     a.bias = bias;
@@ -448,13 +438,13 @@ extern "C" int corey_conv_packed_bwd(const void* x, int64_t x_stride, const floa
     a.D = (int32_t)D;
     a.pieces = (int32_t)l.max_blocks;
     a.parts = static_cast<float*>(workspace);
-    a.groups = (int32_t)((D + wide - 1) / wide);
+    a.groups = (int32_t)groups_of(D);
     a.runs = (int32_t)runs_of(l.max_blocks, a.groups, &a.run);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const unsigned grid = (unsigned)((a.runs + kWaves - 1) / kWaves * a.groups);
-    by_backward_width(dt, D, [&](auto t, auto v) {
-        by_taps(W, [&](auto w) {
-            k_conv_packed_bwd<decltype(t), decltype(v)::value, decltype(w)::value><<<grid, kThreads, 0, stream>>>(a);
+    by_type(dt, [&](auto t) {
+        by_width(D, [&](auto v) {
+            by_taps(W, [&](auto w) { k_conv_packed_bwd<decltype(t), decltype(v)::value, decltype(w)::value><<<grid, kThreads, 0, stream>>>(a); });
         });
     });
     k_conv_packed_sum<<<(unsigned)(((W + 1) * D + 63) / 64), 64 * kSumWaves, 0, stream>>>(a, W, dweight, dbias);

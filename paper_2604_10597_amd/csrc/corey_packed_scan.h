@@ -245,6 +245,12 @@ template <typename F> void by_groups(int64_t N, F&& f)
     else f(std::integral_constant<int, 8>());
     static_assert(COREY_PACK_MAX_STATE == 8 * kStates, "the widest workgroup holds all states");
 }
+inline int64_t waves_of(int64_t N)        // of a workgroup
+{
+    int64_t waves = 0;
+    by_groups(N, [&](auto g) { waves = Shape<decltype(g)::value>::waves; });
+    return waves;
+}
 
 }  // namespace corey_packed
 #endif

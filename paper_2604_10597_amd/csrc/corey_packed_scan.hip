@@ -334,15 +334,16 @@ __global__ __launch_bounds__(256) void k_packed_step_any(StepArgs a)
 // is begun.
 extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
 {
-    if (S < 1 || T < 1 || D < 1 || N < 1) return 0;
+    if (S < 1 || T < 1 || T > INT32_MAX || D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE) return 0;
     const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16);
     if (backward) {
         // a tile's work is in proportion to its tokens and some for each tile; three waves a SIMD run at once, and a round lasts as long as a
         // tile.  8192 tokens of 2048 channels in 11 sequences: 16, 32, 48, 64 tokens 459, 417, 403, 445 us; 2048 of 1536 116, 128, 163, 168
+        constexpr double kThree = 3. * 4. * 256.;
         int32_t best = 0;
         double least = 0.;
         for (int32_t tile = COREY_PACK_BLOCK; tile <= (N > 64 ? 32 : 64); tile += COREY_PACK_BLOCK) {
-            double rounds = (double)(int64_t)(((double)T / tile + 0.5 * (double)S) * waves / 3072.0 + 0.9);
+            double rounds = (double)(int64_t)(((double)T / tile + 0.5 * (double)S) * waves / kThree + 0.9);
             if (rounds < 1.) rounds = 1.;
             const double cost = rounds * (tile + 8);
             if (best == 0 || cost < least) best = tile, least = cost;
@@ -414,7 +415,7 @@ extern "C" int corey_scan_packed(const void* u, int64_t u_stride, const void* de
     a.blocks = (int32_t)l.max_blocks;
     a.groups = (int32_t)channel_groups(D, N);
     const int64_t grid = l.max_tiles * a.groups, columns = (D * N + 255) / 256, relay = (l.max_blocks * N * 32 + 255) / 256;
-    if (grid > INT32_MAX || relay > INT32_MAX || columns * (l.max_longs + 1) > INT32_MAX) return fail(COREY_ESHAPE, "%s: T * D is too large", who);
+    if (!good_grid(grid, 64 * waves_of(N)) || !good_grid(relay, 256) || !good_grid(columns * l.max_longs, 256)) return fail(COREY_ESHAPE, "%s: T * D is too large", who);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dt, [&](auto t) {
         using T = decltype(t);

@@ -562,7 +562,7 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
     a.groups = (int32_t)channel_groups(D, N);
     const int64_t columns = (D * N + 255) / 256, groups = channel_groups(D, N);
     const int64_t relay = (l.max_blocks * N * 32 + 255) / 256;
-    if (l.max_tiles * groups > INT32_MAX || 2 * columns * (l.max_longs + 1) > INT32_MAX || relay > INT32_MAX)
+    if (!good_grid(l.max_tiles * groups, 64 * waves_of(N)) || !good_grid(2 * columns * l.max_longs, 256) || !good_grid(relay, 256))
         return fail(COREY_ESHAPE, "%s: T * D is too large", who);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     by_type(dt, [&](auto t) {

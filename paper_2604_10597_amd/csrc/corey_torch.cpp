@@ -861,10 +861,13 @@ PyObject* pack_part(PyObject* const* a)      // pack, part
     const int64_t part = integer(a[1]);
     const Owned o(PyObject_GetAttrString(a[0], "table"));
     if (!o.o) throw PyError{};
-    const at::Tensor& t = tensor(o.o, "pack.table");
+    const at::Tensor* table = any_tensor(o.o, "pack.table");
+    if (!table) raise(PyExc_TypeError, "%s must be a tensor", "pack.table");
+    const at::Tensor& t = *table;
     const auto up = [](int64_t n) { return (n + 3) / 4 * 4; };
     const auto pieces = [&](int64_t size) { return p->T / size + (p->S < p->T ? p->S : p->T); };
-    if (p->tile < 1 || t.data_ptr() != p->table || t.nbytes() < p->bytes) raise(PyExc_ValueError, "pack is not as corey_pack_plan left it");
+    if (p->tile < 1 || t.data_ptr() != p->table || t.nbytes() < p->bytes || t.scalar_type() != at::kInt)
+        raise(PyExc_ValueError, "pack is not as corey_pack_plan left it");
     const int64_t starts = 16, seq = starts + up(p->S + 1), tiles = seq + up(p->T), blocks = tiles + 4 * pieces(p->tile), from = t.storage_offset();
     if (part == 0) return wrap(t.as_strided({p->S + 1}, {1}, from + starts));
     if (part == 1) return wrap(t.as_strided({p->T}, {1}, from + seq));
