@@ -355,8 +355,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             grads[n * 64] = gn;
             shares[n * 64] = an;
         }
-        // what only the end needs is read again (from the cache): kept, it would take the registers of a state's work
-        request(b, count);
+        // what only the gate's gradient needs is read again (from the cache): kept, it would take the registers of a state's work
         if constexpr (GATED) request_rest(b, count);
         if (mine > 0) put_fold(mine - 1, fold_sum(fold_read(rows, lane)), fold_sum(fold_read(rows + kFoldRows, lane)));
         if constexpr (GROUPS == 1) {                             // dB and dC of the block, over the workgroup's channels
