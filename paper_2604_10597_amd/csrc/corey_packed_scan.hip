@@ -15,6 +15,9 @@
 // read the slot before any tile writes it.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "corey_packed_scan.h"
 
 namespace {
@@ -329,31 +332,30 @@ __global__ __launch_bounds__(256) void k_packed_step_any(StepArgs a)
 
 }  // namespace
 
-// Tiles are what runs side by side: some 4.5 waves of 64 channels and 16 states a SIMD, and half a tile a sequence for the ends that fill
-// none.  Shorter tiles mean more begun states to form and to carry, longer ones idle SIMDs (one sequence of 16384 tokens, 5120 channels:
-// tiles of 64, 128, 192 ... 320, 512, 1024 tokens 553, 459, 455, 543, 777 us).  With many sequences a tile takes whole ones and nothing
-// is begun.
+// Tiles are what runs side by side.  A tile costs its tokens and some more for the state it begins with; a SIMD with m waves takes m
+// times that, and more than its share with fewer than four (nothing issues beside them); and a sequence's tiles are chained one after
+// another.  Of the tiles of whole blocks the one with the least of it, counting half a tile a sequence for the ends that fill none.  One
+// sequence of 16384 tokens, 5120 channels: 320 (four waves a SIMD); tiles of 64, 128, 192, 256, 288, 320, 384, 512, 1024 tokens take 467,
+// 440, 451, 456, 499, 456, 529, 545, 777 us.  Where half a tile a sequence fills the GPU a tile takes whole sequences and nothing is begun.
 extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
 {
     if (S < 1 || T < 1 || T > INT32_MAX || D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE) return 0;
-    const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16);
-    if (backward) {
-        // a tile's work is in proportion to its tokens and some for each tile; three waves a SIMD run at once, and a round lasts as long as a
-        // tile.  8192 tokens of 2048 channels in 11 sequences: 16, 32, 48, 64 tokens 459, 417, 403, 445 us; 2048 of 1536 116, 128, 163, 168
-        constexpr double kThree = 3. * 4. * 256.;
-        int32_t best = 0;
-        double least = 0.;
-        for (int32_t tile = COREY_PACK_BLOCK; tile <= (N > 64 ? 32 : 64); tile += COREY_PACK_BLOCK) {
-            double rounds = (double)(int64_t)(((double)T / tile + 0.5 * (double)S) * waves / kThree + 0.9);
-            if (rounds < 1.) rounds = 1.;
-            const double cost = rounds * (tile + 8);
-            if (best == 0 || cost < least) best = tile, least = cost;
-        }
-        return best;
-    }
-    const double fit = 4608.0 / waves, room = fit - 0.5 * (double)S, tile = room >= 1.0 ? (double)T / room : 1024.0;
-    if (tile >= 1024.0) return 1024;
-    return ((int32_t)tile / COREY_PACK_BLOCK + 1) * COREY_PACK_BLOCK;
+    constexpr double kSimds = 4. * 256.;
+    const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16), length = (double)T / (double)S;
+    // backward: three waves a SIMD at once, and a round lasts as long as a tile.  8192 tokens of 2048 channels in 11 sequences: 16, 32, 48,
+    // 64 tokens 459, 417, 403, 445 us; 2048 of 1536 116, 128, 163, 168
+    const auto cost = [&](double tile) {
+        const double fill = (T / tile + 0.5 * S) * waves / kSimds;
+        if (backward) return std::max(1., std::floor(fill / 3. + 0.9)) * (tile + 8.) + 0.07 * length / tile;
+        const double m = std::max(1., std::ceil(fill - 0.1));
+        return (m == 1. ? 1.75 : m == 2. ? 2.3 : m) * (tile + 6.) + 0.6 * length / tile;
+    };
+    if (!backward && 0.5 * S * waves >= 4.5 * kSimds) return 1024;
+    const int32_t most = !backward ? 1024 : N > 64 ? 32 : 64;
+    int32_t best = COREY_PACK_BLOCK;
+    for (int32_t tile = 2 * COREY_PACK_BLOCK; tile <= most; tile += COREY_PACK_BLOCK)
+        if (cost(tile) < cost(best)) best = tile;
+    return best;
 }
 
 namespace {
