@@ -1,9 +1,10 @@
 /*
  * corey.h -- C ABI of libcorey: the COREY hot path on one AMD MI355X (gfx950).
  *
- * Three operations (and, at the end, the layer's steps on packed batches with their gradients), named after the paper's statement of the problem (its inline scheduling hook runs
+ * Three operations, named after the paper's statement of the problem (its inline scheduling hook runs
  * them in this order on every Mamba layer: statistic of the post-convolution tensor u -> chunk -> scan
- * with that chunk, "Active-Mode Overhead Budget", steps (2)-(4)):
+ * with that chunk, "Active-Mode Overhead Budget", steps (2)-(4)), what surrounds them in a layer, and at
+ * the end the layer's steps on packed batches with their gradients:
  *
  *   corey_entropy_hist   fixed-bin histogram of a tensor, its Shannon entropy H (Eq. 1) and the
  *                        normalised signal r = H / log K (Method, Preliminaries).

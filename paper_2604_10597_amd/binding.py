@@ -372,14 +372,16 @@ def corey_conv_packed(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
 
 def corey_conv_packed_bwd(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None, du: torch.Tensor, pack: Pack,
                           workspace: torch.Tensor | None = None):
-    """Gradients of corey_conv_packed without slots: (dx [T, D], dweight float32 [D, W], dbias float32 [D])."""
+    """Gradients of corey_conv_packed without slots: (dx [T, D], dweight float32 [D, W], dbias float32 [D]).  The rows of dx behind the last
+    sequence hold whatever the memory held."""
     return (_ext or _native()).corey_conv_packed_bwd(x, weight, bias, du, pack, workspace)
 
 
 def corey_scan_packed(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor, Cm: torch.Tensor, pack: Pack, Dv=None, z=None,
                       delta_bias=None, delta_softplus: bool = True, state=None, slots=None, slots_out=None, y=None, workspace=None) -> torch.Tensor:
     """selective_scan_fwd on a packed batch: u, delta, z [T, D], Bm, Cm [T, N] (rows any distance apart), A float32 [D, N]; state float32
-    [slots, D, N], slots and slots_out int32 [S] as in include/corey.h.  Returns y [T, D]."""
+    [slots, D, N], slots and slots_out int32 [S] as in include/corey.h.  Returns y [T, D]; of a y allocated here the rows behind the last
+    sequence hold whatever the memory held."""
     return (_ext or _native()).corey_scan_packed(u, delta, A, Bm, Cm, pack, Dv, z, delta_bias, delta_softplus, state, slots, slots_out, y, workspace)
 
 
@@ -394,5 +396,5 @@ def corey_scan_packed_bwd(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor,
                           workspace=None) -> dict:
     """Gradients of corey_scan_packed without slots, from dy and its inputs: dict(du, ddelta, dA, dB, dC and, where the input was
     given, dD, dz, ddelta_bias).  `pack`: of tile 64 at most, 32 for N > 64 (corey_pack_tile with backward).  `out`: a dict whose tensors are
-    written (missing ones are allocated)."""
+    written (missing ones are allocated: of those the rows behind the last sequence hold whatever the memory held)."""
     return (_ext or _native()).corey_scan_packed_bwd(u, delta, A, Bm, Cm, pack, dy, Dv, z, delta_bias, delta_softplus, out, workspace)

@@ -4,8 +4,9 @@
 //
 // Channels lie side by side in memory, so a lane is a channel and walks the tokens one after another: B and C of a token are the same
 // for the whole wave and sit in scalar registers, the states stay in vector registers, and nothing is exchanged between lanes.  Per
-// token, channel and state that is one exponential and four plain instructions; a SIMD issues the first in 8 cycles, the others in 2,
-// so vector issue is the bound (memory moves 8 bytes per token and channel in 16-bit storage).
+// token, channel and state that is one exponential and four plain instructions; a SIMD issues the first in 8.4 cycles, the others in 2.3
+// where two waves' pair, 4.3 where they do not, so vector issue is the bound (memory moves 8 bytes per token and channel in 16-bit
+// storage).
 //
 // Long sequences are cut into tiles that are walked side by side:
 //   k_packed_ends    every tile but a sequence's last, from a zero state: its end state E and the sum of its step sizes
@@ -13,6 +14,10 @@
 //   k_packed_scan    every tile from that state; the last one leaves the sequence's state in its slot
 // Sequences of one tile need the last kernel alone: its wave reads the slot before it writes it.  In longer ones k_packed_chain has
 // read the slot before any tile writes it.
+//
+// One sequence of 16384 tokens of 5120 bf16 channels with 16 states and a gate, us: 278 for k_packed_scan, of which the states' work takes
+// 176 at the 148 cycles that a state and 8 tokens of a wave take in a loop by themselves (corey_packed_scan.h), the rest is step sizes,
+// gates, loads and stores and what waits; 204 for k_packed_ends, 13 for k_packed_chain, 5 for the relay of B and C.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -80,7 +85,8 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_ends(Pa
     if (n0 == 0) a.sums[(int64_t)tile * a.D + d] = sum;
 }
 
-// A lane is one channel and state of one sequence.  The tiles' values are requested kAhead at a time.
+// A lane is one channel and state of one sequence.  The tiles' values are requested kAhead at a time (48 sequences of up to 64 tiles, 2048
+// channels, us: 8 19, 16 21, 32 27).
 constexpr int kAhead = 8;
 __global__ __launch_bounds__(256) void k_packed_chain(PackedScanArgs a, int columns)
 {
