@@ -40,7 +40,9 @@ struct PackedScanArgs {
     float *dA, *dD, *dbias;
     int64_t dy_stride, du_stride, dd_stride, dz_stride, db_stride, dc_stride;
     float* backs;                         // workspace [tiles, N, D]: what a tile hands to the gradient of the state it begins with
-    float* starts;                        // workspace [tiles, tile / 16 - 1, N, D]: the states that a tile's blocks 1, 2, ... begin with
+    float* starts;                        // workspace [tiles, tile / 16 - 1, N, D]: the states that a tile's blocks 1, 2, ... begin with when
+                                          // the tile begins from zero
+    float* start_sums;                    // workspace [tiles, tile / 16 - 1, D]: the sums of the step sizes before them
     float* part_bc;                       // workspace [channel groups, blocks, N, 16 tokens, (dB, dC)]
     float* part_a;                        // workspace [tiles, N + 2, D]: dA, dD and dbias of a tile
 };

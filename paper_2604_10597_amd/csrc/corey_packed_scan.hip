@@ -348,13 +348,12 @@ extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, i
     if (S < 1 || T < 1 || T > INT32_MAX || D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE) return 0;
     constexpr double kSimds = 4. * 256.;
     const double waves = (double)((D + 63) / 64) * (double)((N + 15) / 16), length = (double)T / (double)S;
-    // backward: three waves a SIMD at once, and a round lasts as long as a tile.  8192 tokens of 2048 channels in 11 sequences: 16, 32, 48,
-    // 64 tokens 459, 417, 403, 445 us; 2048 of 1536 116, 128, 163, 168
+    // backward: 8192 tokens of 2048 bf16 channels in 11 sequences, tiles of 16, 32, 48, 64 tokens 477, 375, 338, 370 us; 2048 of 1536 in
+    // four 112, 99, 124, 130; 16384 of 4096 in four 1682, 1312, 1199, 1167; 16384 of 64 in one 233, 157, 158, 156
+    const double more = backward ? 8. : 6., chained = backward ? 0.15 : 0.6, slack = backward ? 0. : 0.1;
     const auto cost = [&](double tile) {
-        const double fill = (T / tile + 0.5 * S) * waves / kSimds;
-        if (backward) return std::max(1., std::floor(fill / 3. + 0.9)) * (tile + 8.) + 0.07 * length / tile;
-        const double m = std::max(1., std::ceil(fill - 0.1));
-        return (m == 1. ? 1.75 : m == 2. ? 2.3 : m) * (tile + 6.) + 0.6 * length / tile;
+        const double m = std::max(1., std::ceil((T / tile + 0.5 * S) * waves / kSimds - slack));
+        return (m == 1. ? 1.75 : m == 2. ? 2.3 : m) * (tile + more) + chained * length / tile;
     };
     if (!backward && 0.5 * S * waves >= 4.5 * kSimds) return 1024;
     const int32_t most = !backward ? 1024 : N > 64 ? 32 : 64;

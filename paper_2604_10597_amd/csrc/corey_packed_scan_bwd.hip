@@ -5,18 +5,19 @@
 //     dC_t = sum_d ds h,  dB_t = sum_d g dl u,  ddl = sum_n g (u B + A a h_{t-1}),  du = D ds + dl sum_n g B,  dA = sum_t g dl a h_{t-1}
 //
 // Sequences are cut into tiles of at most 64 tokens that are walked side by side:
-//   k_packed_bwd_ends   every tile of a longer sequence: its end state E from zero, the gradient G that it hands to the state it begins
-//                       with when none comes from behind, and the sum of its step sizes
+//   k_packed_bwd_ends   every tile of more than one block of 16 tokens or of a longer sequence: its end state E from zero, those at
+//                       the starts of its blocks, the gradient G that it hands to the state it begins with when none comes from
+//                       behind, and the sums of its step sizes
 //   k_packed_bwd_chain  per sequence, over its tiles: forward h_k+1 = exp(A sum) h_k + E_k, backward g_k-1 = exp(A sum) g_k + G_k
-//   k_packed_bwd        every tile: the states at the starts of its blocks of 16 tokens (kept in the workspace), then block by block
-//                       from the last, state by state: the block's decays and states forward, its gradients backward.  Sums over
-//                       states stay in the lane (a lane is a channel); sums over channels (dB, dC) are folded over the wave's lanes,
-//                       over the workgroup's waves in LDS, and written per workgroup
+//   k_packed_bwd        every tile, block by block from the last, state by state: the block begins with exp(A sum) times the tile's first
+//                       state and its own from zero; from there the block's decays and states forward, its gradients backward.
+//                       Sums over states stay in the lane (a lane is a channel); sums over channels (dB, dC) are folded over the
+//                       wave's lanes, over the workgroup's waves in LDS, and written per workgroup
 //   k_packed_bwd_bc, k_packed_bwd_a   add up the workgroups' dB and dC, and the tiles' dA, dD and dbias, always in the same order
-// Per token, channel and state k_packed_bwd issues 25 vector instructions, two of them exponentials, and k_packed_bwd_ends 8; vector
-// issue is the bound, two waves a SIMD (205 registers and 19 KB of LDS a wave).  8192 tokens of 2048 bf16 channels with 16 states in 11 sequences,
-// us: 308 (vector issue fills two thirds of the SIMDs' cycles; by leaving parts out: the folds 45, the states at block starts 50, the
-// end of a block with its stores 50), ends 74, chain 20, dA 8, dB and dC 7, relay 5.
+// Per token, channel and state k_packed_bwd issues some 21 vector instructions, one of them an exponential, and k_packed_bwd_ends 8; vector
+// issue is the bound, two waves a SIMD (216 registers and 19 KB of LDS a wave).  8192 tokens of 2048 bf16 channels with 16 states in 11
+// sequences, us: 254, ends 85, chain 21, dA 8, dB and dC 8, relay 5.  (With the states at block starts formed again in k_packed_bwd 308 and
+// ends 74.  Leaving parts out: the folds take 45, a block's end with its stores 50.)
 #include <hip/hip_runtime.h>
 
 #include "corey_packed_scan.h"
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
     const int n0 = GROUPS > 1 ? wave * kStates : 0;
     const int tile = (int)(blockIdx.x / (unsigned)a.groups);
     const Piece p = a.ix.tiles[tile];
-    if (!a.ix.good() || p.seq < 0 || p.bits == 3 || n0 >= a.N) return;
+    if (!a.ix.good() || p.seq < 0 || (p.bits == 3 && p.count <= kTok) || n0 >= a.N) return;
     const int d = (int)(blockIdx.x % (unsigned)a.groups) * Shape<GROUPS>::channels + (GROUPS > 1 ? 0 : wave * 64) + lane;
     if (d >= a.D) return;
     const uint32_t off = (uint32_t)d * (uint32_t)sizeof(T);
@@ -66,8 +67,17 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
     }
     const float bias = a.bias ? a.bias[d] : 0.f;
     const float* from = a.bc + (first_block(a.ix, p) * 2 * a.N + n0) * 2 * kHalf;
+    const int64_t starts = (int64_t)tile * (a.ix.tile / kTok - 1);
     for (int t0 = 0; t0 < p.count; t0 += K) {
         const int count = p.count - t0;
+        if (t0 != 0 && t0 % kTok == 0) {                         // a block but the tile's first begins
+            const int64_t at = starts + t0 / kTok - 1;
+            float* start = a.starts + (at * a.N + n0) * a.D + d;
+#pragma unroll
+            for (int n = 0; n < kStates; ++n)
+                if (n0 + n < a.N) start[(int64_t)n * a.D] = h[n];
+            if (n0 == 0) a.start_sums[at * a.D + d] = sum;
+        }
         StatePairs s(from);
         float dl[K], dx[K], ds[K];
         steps<T, K>(u, delta, bias, a.softplus != 0, count, dl, dx);
@@ -98,6 +108,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
         }
         from += a.N * 2 * kHalf;
     }
+    if (p.bits == 3) return;
     const int64_t at = ((int64_t)tile * a.N + n0) * a.D + d;
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
@@ -187,8 +198,8 @@ __device__ __forceinline__ float fold_sum(const Quarter& q)
 }
 
 // The loop over the states is a loop (unrolled it is 50 KB of instructions, more than the instruction cache feeds), so what belongs to
-// a state from block to block stays out of registers: its gradient and its share of dA in LDS, per lane, and its value at the starts
-// of the blocks in the workspace (in LDS it would halve the waves of a SIMD).
+// a state from block to block stays out of registers: its gradient and its share of dA in LDS, per lane, its value at the starts
+// of the blocks in the workspace.
 template <typename T, bool GATED, int GROUPS>
 __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(PackedScanArgs a)
 {
@@ -218,7 +229,9 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
     const float* arow = a.A + (int64_t)d * a.N + safe;
     const float* first_states = a.ends + ((int64_t)tile * a.N + safe) * a.D + d;
     const int64_t slab = (int64_t)a.N * a.D;
-    float* starts = a.starts + ((int64_t)tile * (a.ix.tile / kTok - 1) * a.N + safe) * a.D + d;
+    const int64_t starts_at = (int64_t)tile * (a.ix.tile / kTok - 1);
+    const float* starts = a.starts + (starts_at * a.N + safe) * a.D + d;
+    const float* start_sums = a.start_sums + starts_at * a.D + d;
     float* part = a.part_a + ((int64_t)tile * (a.N + 2) + safe) * a.D + d;
     const bool begins = (p.bits & 1) != 0;                       // the sequence begins here, from zero
     float* rows = s_mem[wave];
@@ -240,47 +253,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
         if constexpr (GATED) z = load_tokens<T, kTok>(Rows<T>(a.z, a.z_stride, first), count, off);
     };
     const int last_count = p.count - (blocks - 1) * kTok;
-    request(0, blocks > 1 ? kTok : last_count);
-
-    // forward over all blocks but the last: the states that blocks 1, 2, ... begin with.  (A log2(e) lies where rows are folded later: a
-    // global load in this loop would be waited for together with the next block's tokens.)
-    if (blocks > 1) {
-        float* decays = rows + lane;
-        float row[kStates];
-        load_row<kStates>(row, arow, safe, a.N);
-#pragma unroll
-        for (int n = 0; n < kStates; ++n) decays[n * 64] = row[n] * kLog2e;
-#pragma unroll 4
-        for (int n = 0; n < mine; ++n) grads[n * 64] = begins ? 0.f : first_states[(int64_t)n * a.D];
-        for (int b = 0; b + 1 < blocks; ++b) {
-            float dl[kTok], dx[kTok];
-            const float* from = bc + (int64_t)b * 2 * half;
-            float a_next = decays[0];
-            State8 s_next[2] = {state8(from), state8(from + half)};
-            steps<T, kTok>(u, delta, bias, sp, kTok, dl, dx);
-            request(b + 1, b + 2 < blocks ? kTok : last_count);
-#pragma unroll 1
-            for (int n = 0; n < mine; ++n) {
-                const int m = min(n + 1, mine - 1);
-                const float a2 = a_next;
-                a_next = decays[m * 64];
-                float h = grads[n * 64];
-                float e[kTok];
-#pragma unroll
-                for (int t = 0; t < kTok; ++t) e[t] = dl[t] * a2;
-                __builtin_amdgcn_sched_barrier(0);
-                exp2_burst<kTok>(e);
-                __builtin_amdgcn_sched_barrier(0);
-                const State8 s[2] = {s_next[0], s_next[1]};
-                s_next[0] = state8(from + m * 2 * kHalf);
-                s_next[1] = state8(from + m * 2 * kHalf + half);
-#pragma unroll
-                for (int t = 0; t < kTok; ++t) h = fmaf(e[t], h, dx[t] * s[t / kHalf].b(t % kHalf));
-                grads[n * 64] = h;
-                if (on) starts[b * slab + (int64_t)n * a.D] = h;
-            }
-        }
-    }
+    request(blocks - 1, last_count);
     request_rest(blocks - 1, last_count);
 
 #pragma unroll 4
@@ -305,10 +278,10 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             gb[t] = gk[t] = out[t] = 0.f;
         }
         const int64_t place = ((int64_t)group * a.blocks + block0 + b) * a.N + safe;
-        // the states the block begins with
-        const float* begin = b > 0 ? starts + (b - 1) * slab : first_states;
-        const bool zero = b == 0 && begins;
-        float a_next = arow[0], h_next = zero ? 0.f : begin[0];
+        // the states the block begins with: the tile's first ones, decayed, and the block's from zero
+        const float* begin = starts + (b - 1) * slab;
+        const float before = b > 0 ? start_sums[(b - 1) * (int64_t)a.D] : 0.f;
+        float a_next = arow[0], f_next = begins ? 0.f : first_states[0], h_next = b > 0 ? begin[0] : 0.f;
         // a token's sums of dB and dC of state n: four lanes hold both, the even ones put the first in its place, the odd ones the second
         const auto put_fold = [&](int n, float sum_b, float sum_c) {
             const float sum = (lane & 1) ? sum_c : sum_b;
@@ -321,7 +294,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             // What LDS has for this state and the folded rows of the one before are asked for ahead of the exponentials; behind them
             // comes the wait for all of it and for the scalar loads (they count together), and then the next scalar loads go out.
             const float a2 = a_next * kLog2e;
-            float h = h_next, gn = grads[n * 64], an = shares[n * 64];
+            float h = fmaf(fast_exp2(before * a2), f_next, h_next), gn = grads[n * 64], an = shares[n * 64];
             const Quarter before_b = fold_read(rows, lane), before_c = fold_read(rows + kFoldRows, lane);
             float e[kTok], w[kTok], v[kTok];
 #pragma unroll
@@ -333,7 +306,8 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             const int m = min(n + 1, mine - 1);
             put_fold(max(n - 1, 0), fold_sum(before_b), fold_sum(before_c));     // (of the first state: of what is there, overwritten by the next)
             a_next = arow[m];
-            h_next = zero ? 0.f : begin[(int64_t)m * a.D];
+            f_next = begins ? 0.f : first_states[(int64_t)m * a.D];
+            h_next = b > 0 ? begin[(int64_t)m * a.D] : 0.f;
             s_next[0] = state8(from + m * 2 * kHalf);
             s_next[1] = state8(from + m * 2 * kHalf + half);
 #pragma unroll
@@ -487,7 +461,7 @@ __global__ __launch_bounds__(256) void k_packed_bwd_a(PackedScanArgs a)
 
 // The workspace's parts, in floats.
 struct Space {
-    int64_t bc, ends, backs, sums, starts, part_bc, part_a, all;
+    int64_t bc, ends, backs, sums, starts, start_sums, part_bc, part_a, all;
 };
 Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
 {
@@ -499,7 +473,8 @@ Space space(const Layout& l, int64_t T, int32_t tile, int64_t D, int64_t N)
     s.backs = s.ends + tiles * N * D;
     s.sums = s.backs + tiles * N * D;
     s.starts = s.sums + tiles * D;
-    s.part_bc = s.starts + l.max_tiles * (tile / kTok - 1) * N * D;
+    s.start_sums = s.starts + l.max_tiles * (tile / kTok - 1) * N * D;
+    s.part_bc = s.start_sums + l.max_tiles * (tile / kTok - 1) * D;
     s.part_a = s.part_bc + groups * l.max_blocks * 32 * N;
     s.all = s.part_a + l.max_tiles * (N + 2) * D;
     return s;
@@ -557,7 +532,7 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
     a.du = du; a.ddelta = ddelta; a.dz = dz; a.dB = dB; a.dC = dC;
     a.du_stride = du_stride; a.dd_stride = ddelta_stride; a.dz_stride = dz_stride; a.db_stride = dB_stride; a.dc_stride = dC_stride;
     a.dA = dA; a.dD = dDv; a.dbias = ddelta_bias;
-    a.bc = ws + w.bc; a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.starts = ws + w.starts; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
+    a.bc = ws + w.bc; a.ends = ws + w.ends; a.backs = ws + w.backs; a.sums = ws + w.sums; a.starts = ws + w.starts; a.start_sums = ws + w.start_sums; a.part_bc = ws + w.part_bc; a.part_a = ws + w.part_a;
     a.D = (int32_t)D; a.N = (int32_t)N;
     a.softplus = delta_softplus ? 1 : 0;
     a.blocks = (int32_t)l.max_blocks;
@@ -574,10 +549,8 @@ extern "C" int corey_scan_packed_bwd(const void* u, int64_t u_stride, const void
             const auto go = [&](auto gate, auto whole) {
                 constexpr bool Z = decltype(gate)::value;
                 k_packed_relay<T><<<(unsigned)relay, 256, 0, stream>>>(a);
-                if (pack->T > pack->tile) {
-                    k_packed_bwd_ends<T, Z, G, decltype(whole)::value><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
-                    k_packed_bwd_chain<<<(unsigned)(2 * columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
-                }
+                if (pack->T > kTok) k_packed_bwd_ends<T, Z, G, decltype(whole)::value><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
+                if (pack->T > pack->tile) k_packed_bwd_chain<<<(unsigned)(2 * columns * l.max_longs), 256, 0, stream>>>(a, (int)columns);
                 k_packed_bwd<T, Z, G><<<(unsigned)(l.max_tiles * groups), 64 * Shape<G>::waves, 0, stream>>>(a);
             };
             const auto with = [&](auto gate) {
