@@ -227,13 +227,18 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
     const float* bc = a.bc + (block0 * 2 * a.N + safe) * 2 * kHalf;
     const int half = a.N * 2 * kHalf;                            // from one half of a block to the next
     const float* arow = a.A + (int64_t)d * a.N + safe;
-    const float* first_states = a.ends + ((int64_t)tile * a.N + safe) * a.D + d;
+    // where there is nothing to read (the sequence begins here, or the block is the tile's first) some finite value is read and counts 0:
+    // a branch there would keep the compiler from asking early
+    const float* some = reinterpret_cast<const float*>(a.ix.head);
+    const bool begins = (p.bits & 1) != 0;                       // the sequence begins here, from zero
+    const float* first_states = begins ? some : a.ends + ((int64_t)tile * a.N + safe) * a.D + d;
+    const int64_t first_step = begins ? 0 : a.D;
+    const float first_there = begins ? 0.f : 1.f;
     const int64_t slab = (int64_t)a.N * a.D;
     const int64_t starts_at = (int64_t)tile * (a.ix.tile / kTok - 1);
     const float* starts = a.starts + (starts_at * a.N + safe) * a.D + d;
     const float* start_sums = a.start_sums + starts_at * a.D + d;
     float* part = a.part_a + ((int64_t)tile * (a.N + 2) + safe) * a.D + d;
-    const bool begins = (p.bits & 1) != 0;                       // the sequence begins here, from zero
     float* rows = s_mem[wave];
     float* grads = rows + kRows + lane;
     float* shares = grads + kKept;
@@ -268,7 +273,23 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
         const int next = max(b - 1, 0), next_count = b > 0 ? kTok : count;       // (behind the first block: the same rows again, for nothing)
         float dl[kTok], dx[kTok], ds[kTok], gb[kTok], gk[kTok], out[kTok];
         const float* from = bc + (int64_t)b * 2 * half;
-        State8 s_next[2] = {state8(from), state8(from + half)};
+        // what a state's work takes from memory
+        struct Ahead {
+            float a, first, h;                                   // A, the tile's first state, the block's from zero
+            State8 s[2];
+        };
+        const float* begin = b > 0 ? starts + (b - 1) * slab : some;
+        const int64_t begin_step = b > 0 ? a.D : 0;
+        const auto ask = [&](int n) {
+            Ahead k;
+            k.a = arow[n];
+            k.first = first_states[n * first_step];
+            k.h = begin[n * begin_step];
+            k.s[0] = state8(from + n * 2 * kHalf);
+            k.s[1] = state8(from + n * 2 * kHalf + half);
+            return k;
+        };
+        Ahead even = ask(0), odd;
         if constexpr (GATED) gates<T, kTok>(z, ds);
         steps<T, kTok>(u, delta, bias, sp, count, dl, dx);
 #pragma unroll
@@ -278,10 +299,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             gb[t] = gk[t] = out[t] = 0.f;
         }
         const int64_t place = ((int64_t)group * a.blocks + block0 + b) * a.N + safe;
-        // the states the block begins with: the tile's first ones, decayed, and the block's from zero
-        const float* begin = starts + (b - 1) * slab;
-        const float before = b > 0 ? start_sums[(b - 1) * (int64_t)a.D] : 0.f;
-        float a_next = arow[0], f_next = begins ? 0.f : first_states[0], h_next = b > 0 ? begin[0] : 0.f;
+        const float before = b > 0 ? start_sums[(b - 1) * (int64_t)a.D] : 0.f, inside = b > 0 ? 1.f : 0.f;
         // a token's sums of dB and dC of state n: four lanes hold both, the even ones put the first in its place, the odd ones the second
         const auto put_fold = [&](int n, float sum_b, float sum_c) {
             const float sum = (lane & 1) ? sum_c : sum_b;
@@ -289,12 +307,12 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             if constexpr (GROUPS == 1) s_mem[wave][kFoldAt + spot] = sum;
             else a.part_bc[place * 2 * kTok + spot] = sum;
         };
-#pragma unroll 1
-        for (int n = 0; n < mine; ++n) {
+        // One state's work, which asks for the next one's values.
+        const auto state = [&](int n, const Ahead& now, Ahead& next) {
             // What LDS has for this state and the folded rows of the one before are asked for ahead of the exponentials; behind them
             // comes the wait for all of it and for the scalar loads (they count together), and then the next scalar loads go out.
-            const float a2 = a_next * kLog2e;
-            float h = fmaf(fast_exp2(before * a2), f_next, h_next), gn = grads[n * 64], an = shares[n * 64];
+            const float a2 = now.a * kLog2e;
+            float h = fmaf(fast_exp2(before * a2), first_there * now.first, inside * now.h), gn = grads[n * 64], an = shares[n * 64];
             const Quarter before_b = fold_read(rows, lane), before_c = fold_read(rows + kFoldRows, lane);
             float e[kTok], w[kTok], v[kTok];
 #pragma unroll
@@ -302,14 +320,10 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             __builtin_amdgcn_sched_barrier(0);
             exp2_burst<kTok>(e);
             __builtin_amdgcn_sched_barrier(0);
-            const State8 s[2] = {s_next[0], s_next[1]};
-            const int m = min(n + 1, mine - 1);
+            const State8 s[2] = {now.s[0], now.s[1]};
             put_fold(max(n - 1, 0), fold_sum(before_b), fold_sum(before_c));     // (of the first state: of what is there, overwritten by the next)
-            a_next = arow[m];
-            f_next = begins ? 0.f : first_states[(int64_t)m * a.D];
-            h_next = b > 0 ? begin[(int64_t)m * a.D] : 0.f;
-            s_next[0] = state8(from + m * 2 * kHalf);
-            s_next[1] = state8(from + m * 2 * kHalf + half);
+            next = ask(min(n + 1, mine - 1));
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < kTok; ++t) {
                 w[t] = e[t] * h;                                 // a h_{t-1}
@@ -331,7 +345,14 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             fold_put(rows, v, lane);
             grads[n * 64] = gn;
             shares[n * 64] = an;
+        };
+        // Two states a turn, so that what is asked for stays where it arrives: moved at the end of a turn it would be waited for there.
+#pragma unroll 1
+        for (int n = 0; n + 1 < mine; n += 2) {
+            state(n, even, odd);
+            state(n + 1, odd, even);
         }
+        if (mine > 0 && (mine & 1)) state(mine - 1, even, odd);
         // what only the gate's gradient needs is read again (from the cache): kept, it would take the registers of a state's work
         if constexpr (GATED) request_rest(b, count);
         if (mine > 0) put_fold(mine - 1, fold_sum(fold_read(rows, lane)), fold_sum(fold_read(rows + kFoldRows, lane)));
