@@ -15,9 +15,9 @@
 //                       wave's lanes, over the workgroup's waves in LDS, and written per workgroup
 //   k_packed_bwd_bc, k_packed_bwd_a   add up the workgroups' dB and dC, and the tiles' dA, dD and dbias, always in the same order
 // Per token, channel and state k_packed_bwd issues some 21 vector instructions, one of them an exponential, and k_packed_bwd_ends 8; vector
-// issue is the bound, two waves a SIMD (216 registers and 19 KB of LDS a wave).  8192 tokens of 2048 bf16 channels with 16 states in 11
-// sequences, us: 254, ends 85, chain 21, dA 8, dB and dC 8, relay 5.  (With the states at block starts formed again in k_packed_bwd 308 and
-// ends 74.  Leaving parts out: the folds take 45, a block's end with its stores 50.)
+// issue is the bound, two waves a SIMD (some 240 registers and 19 KB of LDS a wave).  8192 tokens of 2048 bf16 channels with 16 states in 11
+// sequences, us: 241, ends 85, chain 21, dA 8, dB and dC 8, relay 5.  (With the states at block starts formed again in k_packed_bwd 308 and
+// ends 74; before its loop took two states a turn 254.  Leaving parts out: the folds take 45, a block's end with its stores 50.)
 #include <hip/hip_runtime.h>
 
 #include "corey_packed_scan.h"
