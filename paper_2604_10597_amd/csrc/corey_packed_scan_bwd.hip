@@ -299,7 +299,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             gb[t] = gk[t] = out[t] = 0.f;
         }
         const int64_t place = ((int64_t)group * a.blocks + block0 + b) * a.N + safe;
-        const float before = b > 0 ? start_sums[(b - 1) * (int64_t)a.D] : 0.f, inside = b > 0 ? 1.f : 0.f;
+        const float before = b > 0 && !begins ? start_sums[(b - 1) * (int64_t)a.D] : 0.f, inside = b > 0 ? 1.f : 0.f;
         // a token's sums of dB and dC of state n: four lanes hold both, the even ones put the first in its place, the odd ones the second
         const auto put_fold = [&](int n, float sum_b, float sum_c) {
             const float sum = (lane & 1) ? sum_c : sum_b;

@@ -200,6 +200,52 @@ def test_a_sequence_of_nan_keeps_it_to_itself():
     assert torch.equal(pool[0], pool2[0]) and torch.equal(pool[2], pool2[2])
 
 
+@pytest.mark.parametrize("N, tile", [(21, 16), (21, 64), (50, 48), (35, 32), (127, 32), (3, 64)])
+def test_states_that_fill_no_wave(N, tile):
+    """Forward and backward with numbers of states that leave a wave's last group of four, its last pair or a whole wave unfilled."""
+    lengths = [40, 1, 0, 70, 16]
+    b = Batch(lengths, 67, N, "f32", seed=N)
+    pack = corey.corey_pack_plan(b.lens(), b.T, tile)
+    y = corey.corey_scan_packed(b.u, b.delta, b.A, b.B, b.C, pack, **scan_kw(b))
+    g = corey.corey_scan_packed_bwd(b.u, b.delta, b.A, b.B, b.C, pack, b.dy, **scan_kw(b))
+    sums = {}
+    for s, (f, e) in enumerate(b.spans):
+        if e == f:
+            continue
+        r = b.scan(s, None, True, tile)
+        ref.check(f64(y[f:e]), *r.forward("f32"), "y")
+        for k, (v, err) in r.backward(b.dy64[f:e], 12, b.T // 16 + 5).items():
+            if k in ("dA", "dD", "ddelta_bias"):
+                old = sums.get(k, (0.0, 0.0))
+                sums[k] = (old[0] + v, old[1] + err)
+            else:
+                ref.check(f64(g[k][f:e]), v, ref.stored(v, err, "f32"), k)
+    for k, (v, err) in sums.items():
+        ref.check(f64(g[k]), v, err + ref.TINY["f32"], k)
+
+
+def test_growing_states_from_zero():
+    """Step sizes below 0 (no softplus): over the first block the decays multiply to more than binary32 holds, but the state there is 0 (B is),
+    so nothing of it may show."""
+    D, N, n = 8, 4, 33
+    b = Batch([n], D, N, "f32", seed=3, gated=False, skip=False, bias=False)
+    b.A64 = -np.ones((D, N))
+    delta = np.full((n, D), 0.1)
+    delta[:16] = -89.2 / 16
+    b.delta, b.delta64 = rounded(delta, "f32")
+    bm = b.B64.copy()
+    bm[:16] = 0.0
+    b.B, b.B64 = rounded(bm, "f32")
+    b.dy, b.dy64 = rounded(1e-6 * b.dy64, "f32")
+    to = lambda t: t.to(DEV)
+    pack = corey.corey_pack_plan(b.lens(), n, 48)
+    g = corey.corey_scan_packed_bwd(b.u, to(b.delta), to(torch.from_numpy(b.A64.astype(np.float32))), to(b.B), b.C, pack, to(b.dy), delta_softplus=False)
+    back = b.scan(0, None, False, 48).backward(b.dy64, 12, 4)
+    for k in ("du", "ddelta", "dB", "dC"):
+        ref.check(f64(g[k]), back[k][0], ref.stored(*back[k], "f32"), k)
+    ref.check(f64(g["dA"]), back["dA"][0], back["dA"][1] + ref.TINY["f32"], "dA")
+
+
 # ------------------------------------------------------------------------------------------- graphs and streams
 def test_two_graphs_replayed_in_turn():
     """Index, convolution, scan and gradients in one graph, generation in another that works on the same pools; replayed in turn with new
