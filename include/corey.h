@@ -427,7 +427,8 @@ int selective_state_update(void* state, const void* x, const void* delta, const 
  *     it is (a prompt's state from which several continuations begin).  No slot may be written for two sequences of a call, or
  *     written for one and read for another: which state is read or kept would be undefined.  A sequence without tokens
  *     leaves both its slots as they are.
- *   - Arithmetic, sums and scan states in binary32; results are rounded once to `dt`.
+ *   - Arithmetic, sums and scan states in binary32; results are rounded once to `dt`.  Decays are multiplied over a tile's tokens: where
+ *     they grow (dl A above 0) their product has to stay within binary32, as a state that grows with them does.
  * ----------------------------------------------------------------------------------------------------- */
 #define COREY_PACK_BLOCK 16               /* tokens of the small pieces                                   */
 #define COREY_PACK_MAX_TILE 2048

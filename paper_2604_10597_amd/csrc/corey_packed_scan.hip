@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void k_packed_chain(PackedScanArgs a, int colu
         for (int i = 0; i < kAhead; ++i) {
             if (k0 + i < stop) {
                 e[(k0 + i) * wide] = h;
-                h = fmaf(fast_exp2(a2 * sum[i]), h, end[i]);
+                h = h == 0.f ? end[i] : fmaf(fast_exp2(a2 * sum[i]), h, end[i]);   // (a decay may have overflowed, step sizes below 0)
             }
         }
     }

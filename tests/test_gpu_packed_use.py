@@ -244,6 +244,12 @@ def test_growing_states_from_zero():
     for k in ("du", "ddelta", "dB", "dC"):
         ref.check(f64(g[k]), back[k][0], ref.stored(*back[k], "f32"), k)
     ref.check(f64(g["dA"]), back["dA"][0], back["dA"][1] + ref.TINY["f32"], "dA")
+    pool = torch.zeros(1, D, N, device=DEV)                      # and over a tile, from a state of 0
+    y = corey.corey_scan_packed(b.u, to(b.delta), to(torch.from_numpy(b.A64.astype(np.float32))), to(b.B), b.C,
+                                corey.corey_pack_plan(b.lens(), n, 16), delta_softplus=False, state=pool, slots=ints(0))
+    r = b.scan(0, None, False, 16)
+    ref.check(f64(y), *r.forward("f32"), "y")
+    ref.check(f64(pool[0]), *r.last(), "state")
 
 
 # ------------------------------------------------------------------------------------------- graphs and streams
