@@ -334,6 +334,39 @@ def test_streams():
             assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("lengths, T, D, N, tile", [([40, 1, 0, 70, 16], 127, 67, 16, 16), ([17], 17, 300, 16, 64), ([64, 64], 128, 130, 40, 32), ([5, 5, 5], 16, 33, 128, 16), ([500], 503, 64, 7, 48)])
+def test_a_workspace_of_the_callers(lengths, T, D, N, tile):
+    """Workspaces, and the table, of exactly the sizes asked for, with whatever they hold: the same results, nothing written behind them."""
+    b = Batch(lengths, D, N, "f32", T=T, seed=1)
+    L, room = binding.lib(), 4096
+
+    def memory(n):
+        whole = torch.randint(0, 256, (n + room,), dtype=torch.uint8, device=DEV)
+        return whole, whole[n:].clone()
+    guards = []
+
+    def exactly(n):
+        whole, behind = memory(n)
+        guards.append((whole[n:], behind))
+        return whole[:n]
+    table = exactly(L.corey_pack_bytes(len(lengths), T, tile)).view(torch.int32)
+    pack, other = corey.corey_pack_plan(b.lens(), T, tile, table=table), corey.corey_pack_plan(b.lens(), T, tile)
+    n = sum(lengths)
+    for x, y in zip((pack.starts, pack.seq, pack.tiles, pack.blocks), (other.starts, other.seq, other.tiles, other.blocks)):
+        assert torch.equal(x, y)
+    y = corey.corey_scan_packed(b.u, b.delta, b.A, b.B, b.C, pack, workspace=exactly(L.corey_scan_packed_workspace(pack, D, N)), **scan_kw(b))
+    assert torch.equal(y[:n], corey.corey_scan_packed(b.u, b.delta, b.A, b.B, b.C, other, **scan_kw(b))[:n])
+    g = corey.corey_scan_packed_bwd(b.u, b.delta, b.A, b.B, b.C, pack, b.dy, workspace=exactly(L.corey_scan_packed_bwd_workspace(pack, D, N)), **scan_kw(b))
+    for k, v in corey.corey_scan_packed_bwd(b.u, b.delta, b.A, b.B, b.C, other, b.dy, **scan_kw(b)).items():
+        assert torch.equal(g[k][:n], v[:n]) if k in ("du", "ddelta", "dz", "dB", "dC") else torch.equal(g[k], v), k
+    w = torch.linspace(-1, 1, 4 * D, device=DEV).reshape(D, 4)
+    mine = corey.corey_conv_packed_bwd(b.u, w, None, b.dy, pack, workspace=exactly(L.corey_conv_packed_bwd_workspace(pack, D, 4)))
+    dx, dw, db = corey.corey_conv_packed_bwd(b.u, w, None, b.dy, other)
+    assert torch.equal(mine[0][:n], dx[:n]) and torch.equal(mine[1], dw) and torch.equal(mine[2], db)
+    for now, before in guards:
+        assert torch.equal(now, before)
+
+
 # ------------------------------------------------------------------------------------------- memory that is no index
 @pytest.mark.parametrize("kind", ["zeros", "noise", "other sizes", "other tile"])
 def test_memory_that_is_no_index_is_not_followed(kind):
