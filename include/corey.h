@@ -428,7 +428,8 @@ int selective_state_update(void* state, const void* x, const void* delta, const 
  *     written for one and read for another: which state is read or kept would be undefined.  A sequence without tokens
  *     leaves both its slots as they are.
  *   - Arithmetic, sums and scan states in binary32; results are rounded once to `dt`.  Decays are multiplied over a tile's tokens: where
- *     they grow (dl A above 0) their product has to stay within binary32, as a state that grows with them does.
+ *     they grow (dl A above 0) their product has to stay within binary32, as a state that grows with them does, unless the state or
+ *     gradient that it multiplies is 0 (that stays 0).
  * ----------------------------------------------------------------------------------------------------- */
 #define COREY_PACK_BLOCK 16               /* tokens of the small pieces                                   */
 #define COREY_PACK_MAX_TILE 2048

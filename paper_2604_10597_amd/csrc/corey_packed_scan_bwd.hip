@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
                 const int r = K - 1 - t;                         // (and the gradients from the last token back)
                 g = fmaf(s.at(n).c(r), ds[r], g) * e[r];
             }
-            back[n] = fmaf(fast_exp2(before * a2[n]), g, back[n]);
+            back[n] = g == 0.f ? back[n] : fmaf(fast_exp2(before * a2[n]), g, back[n]);   // (as in the chain: the decay may have overflowed)
             __builtin_amdgcn_sched_barrier(0);
         }
         from += a.N * 2 * kHalf;
@@ -312,7 +312,8 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
             // What LDS has for this state and the folded rows of the one before are asked for ahead of the exponentials; behind them
             // comes the wait for all of it and for the scalar loads (they count together), and then the next scalar loads go out.
             const float a2 = now.a * kLog2e;
-            float h = fmaf(fast_exp2(before * a2), first_there * now.first, inside * now.h), gn = grads[n * 64], an = shares[n * 64];
+            const float begun = first_there * now.first, own = inside * now.h;
+            float h = begun == 0.f ? own : fmaf(fast_exp2(before * a2), begun, own), gn = grads[n * 64], an = shares[n * 64];
             const Quarter before_b = fold_read(rows, lane), before_c = fold_read(rows + kFoldRows, lane);
             float e[kTok], w[kTok], v[kTok];
 #pragma unroll
