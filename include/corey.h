@@ -464,8 +464,10 @@ int corey_pack_plan(const int32_t* lengths, int64_t S, int64_t T, int32_t tile, 
                     void* hip_stream);
 /* Bytes of table corey_pack_plan needs (0 if the arguments are invalid). */
 size_t corey_pack_bytes(int64_t S, int64_t T, int32_t tile);
-/* A good tile for T rows in S sequences through layers of D channels and N states: as long as enough tiles run side by side; for
- * backward != 0 the one corey_scan_packed_bwd works best with (forward calls take it too).  0 if the arguments are invalid. */
+/* A good tile for T rows in S sequences through layers of D channels and N states: as long as enough tiles run side by side, also where one
+ * sequence is most of the batch.  Of the lengths it knows their mean alone: where many sequences fill the GPU, those of up to four
+ * times that (1024 at most) are walked whole.  For backward != 0 the one corey_scan_packed_bwd works best with (forward calls take it
+ * too).  0 if the arguments are invalid. */
 int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward);
 
 /* corey_conv_packed -- causal_conv1d_silu_fwd on a packed batch: u = v sigmoid(v), v[t] = bias + sum_k weight[k] x[t - (W-1) + k].

@@ -342,7 +342,13 @@ __global__ __launch_bounds__(256) void k_packed_step_any(StepArgs a)
 // times that, and more than its share with fewer than four (nothing issues beside them); and a sequence's tiles are chained one after
 // another.  Of the tiles of whole blocks the one with the least of it, counting half a tile a sequence for the ends that fill none.  One
 // sequence of 16384 tokens, 5120 channels: 320 (four waves a SIMD); tiles of 64, 128, 192, 256, 288, 320, 384, 512, 1024 tokens take 467,
-// 440, 451, 456, 499, 456, 529, 545, 777 us.  Where half a tile a sequence fills the GPU a tile takes whole sequences and nothing is begun.
+// 440, 451, 456, 499, 456, 529, 545, 777 us.
+// Where half a tile a sequence fills the GPU a tile takes whole sequences, up to four times their mean length: cut, they are walked
+// twice (160 sequences of 5120 channels, lengths of 100 spread over a factor of 20, us: 466 in tiles of 272, 328 in one tile each), but one
+// that is much longer than the rest is walked by too few waves if it is not (16384 tokens and 200 sequences of one: 1024 915, 336 some
+// 520, 160 474; 800 and 200 of one: 1024 299, 32 89).  It loses where the longest lies between that and 1024 (exponential lengths of
+// 100: 432 518, 1024 397; spread over a factor of 100: 400 595, 1024 419) and two launches that find nothing to begin (200 sequences of
+// three tokens: 1024 51, 32 58).
 extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, int backward)
 {
     if (S < 1 || T < 1 || T > INT32_MAX || D < 1 || D > COREY_PACK_MAX_CHANNELS || N < 1 || N > COREY_PACK_MAX_STATE) return 0;
@@ -355,8 +361,9 @@ extern "C" int32_t corey_pack_tile(int64_t S, int64_t T, int64_t D, int64_t N, i
         const double m = std::max(1., std::ceil((T / tile + 0.5 * S) * waves / kSimds - slack));
         return (m == 1. ? 1.75 : m == 2. ? 2.3 : m) * (tile + more) + chained * length / tile;
     };
-    if (!backward && 0.5 * S * waves >= 4.5 * kSimds) return 1024;
     const int32_t most = !backward ? 1024 : N > 64 ? 32 : 64;
+    if (!backward && 0.5 * S * waves >= 4.5 * kSimds)
+        return (int32_t)std::min<double>(most, std::max(2., std::ceil(4. * length / COREY_PACK_BLOCK)) * COREY_PACK_BLOCK);
     int32_t best = COREY_PACK_BLOCK;
     for (int32_t tile = 2 * COREY_PACK_BLOCK; tile <= most; tile += COREY_PACK_BLOCK)
         if (cost(tile) < cost(best)) best = tile;
