@@ -214,6 +214,14 @@ template <int C, typename F> __device__ __forceinline__ void arguments(const flo
     exp2_burst<C>(e);
 }
 
+// A for decays in base 2.  Where the product leaves binary32 it stays a number: a step size of 0 (of tokens that are not there) times it
+// is 0, and any other's decay is 0 as well.
+__device__ __forceinline__ float rate(float a)
+{
+    const float r = a * kLog2e;
+    return r == -__builtin_huge_valf() ? -__FLT_MAX__ : r;
+}
+
 // States n0 .. n0 + C - 1 of a row of N in memory; 0 at and behind N.
 template <int C> __device__ __forceinline__ void load_row(float (&out)[C], const float* row, int n0, int N)
 {

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_ends(Pa
     load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
-        a2[n] *= kLog2e;
+        a2[n] = rate(a2[n]);
         h[n] = 0.f;
     }
     const float bias = a.bias ? a.bias[d] : 0.f;
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void k_packed_chain(PackedScanArgs a, int colu
     const int seq = a.ix.longs[which];
     const int first = a.ix.tile_begin[seq], stop = a.ix.tile_begin[seq + 1];
     const int n = (int)(col / a.D), d = (int)(col % a.D);
-    const float a2 = a.A[(int64_t)d * a.N + n] * kLog2e;
+    const float a2 = rate(a.A[(int64_t)d * a.N + n]);
     const int64_t slot = slot_of(a.slots, seq, a.n_slots), wide = (int64_t)a.N * a.D;
     float h = slot >= 0 ? a.state[(slot * a.D + d) * a.N + n] : 0.f;
     float* e = a.ends + col;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_scan(Pa
     float h[kStates], a2[kStates];
     load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
-    for (int n = 0; n < kStates; ++n) a2[n] *= kLog2e;
+    for (int n = 0; n < kStates; ++n) a2[n] = rate(a2[n]);
     const float bias = a.bias ? a.bias[d] : 0.f, skip = a.Dv && n0 == 0 ? a.Dv[d] : 0.f;
     // the state the tile begins with
     if (p.bits == 3) {

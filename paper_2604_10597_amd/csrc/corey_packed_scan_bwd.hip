@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd_end
     load_row<kStates>(a2, a.A + (int64_t)d * a.N + n0, n0, a.N);
 #pragma unroll
     for (int n = 0; n < kStates; ++n) {
-        a2[n] *= kLog2e;
+        a2[n] = rate(a2[n]);
         h[n] = back[n] = 0.f;
     }
     const float bias = a.bias ? a.bias[d] : 0.f;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256) void k_packed_bwd_chain(PackedScanArgs a, int 
     const int seq = a.ix.longs[which];
     const int first = a.ix.tile_begin[seq], stop = a.ix.tile_begin[seq + 1], tiles = stop - first;
     const int n = (int)(col / a.D), d = (int)(col % a.D);
-    const float a2 = a.A[(int64_t)d * a.N + n] * kLog2e;
+    const float a2 = rate(a.A[(int64_t)d * a.N + n]);
     const int64_t wide = (int64_t)a.N * a.D;
     float* e = (forward ? a.ends : a.backs) + col;
     const float* sums = a.sums + d;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * Shape<GROUPS>::waves, 2) void k_packed_bwd(Pac
         const auto state = [&](int n, const Ahead& now, Ahead& next) {
             // What LDS has for this state and the folded rows of the one before are asked for ahead of the exponentials; behind them
             // comes the wait for all of it and for the scalar loads (they count together), and then the next scalar loads go out.
-            const float a2 = now.a * kLog2e;
+            const float a2 = rate(now.a);
             const float begun = first_there * now.first, own = inside * now.h;
             float h = begun == 0.f ? own : fmaf(fast_exp2(before * a2), begun, own), gn = grads[n * 64], an = shares[n * 64];
             const Quarter before_b = fold_read(rows, lane), before_c = fold_read(rows + kFoldRows, lane);

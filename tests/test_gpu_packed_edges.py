@@ -45,3 +45,37 @@ def test_growing_states_from_zero_behind_a_tile(dtype, N):
     for k in ("du", "ddelta", "dB", "dC"):
         ref.check(f64(g[k]), back[k][0], ref.stored(*back[k], dtype), k)
     ref.check(f64(g["dA"]), back["dA"][0], back["dA"][1] + ref.TINY["f32"], "dA")
+
+
+# ------------------------------------------------------------------------------------------- decays of 0
+@pytest.mark.parametrize("value", [-3e38, float("-inf")])
+@pytest.mark.parametrize("N, tile", [(16, 16), (16, 64), (20, 32)])
+def test_states_that_keep_nothing(N, tile, value):
+    """Some of A so far below 0 that its product with log2(e) is no number of binary32 (or that it is none itself): those states hold the last
+    token's product alone.  The tokens that fill up a sequence's last piece have a step size of 0 and change nothing."""
+    lengths, D = [21, 1, 0, 70, 16, 9], 70
+    b = Batch(lengths, D, N, "f32", seed=N + tile)
+    gone = np.random.default_rng(1).random((D, N)) < 0.3
+    b.A64 = np.where(gone, -1e8, b.A64)                          # the reference's: exp(-1e8 dl) is 0 in 64 bits for dl > 8e-6
+    b.A = torch.from_numpy(np.where(gone, value, b.A64).astype(np.float32)).to(DEV)
+    pack = corey.corey_pack_plan(b.lens(), b.T, tile)
+    pool = torch.full((len(lengths), D, N), 9.0, device=DEV)
+    kw = dict(Dv=b.Dv, z=b.z, delta_bias=b.bias)
+    y = corey.corey_scan_packed(b.u, b.delta, b.A, b.B, b.C, pack, state=pool, slots=ints(*[-1] * 6), slots_out=ints(*range(6)), **kw)
+    g = corey.corey_scan_packed_bwd(b.u, b.delta, b.A, b.B, b.C, pack, b.dy, **kw)
+    sums = {}
+    for s, (f, e) in enumerate(b.spans):
+        if e == f:
+            continue
+        r = b.scan(s, None, True, tile)
+        assert r.dl.min() > 8e-6
+        ref.check(f64(y[f:e]), *r.forward("f32"), f"y of sequence {s}")
+        ref.check(f64(pool[s]), *r.last(), f"state of sequence {s}")
+        for k, (v, err) in r.backward(b.dy64[f:e], 12, b.T // 16 + 6).items():
+            if k in ("dA", "dD", "ddelta_bias"):
+                old = sums.get(k, (0.0, 0.0))
+                sums[k] = (old[0] + v, old[1] + err)
+            else:
+                ref.check(f64(g[k][f:e]), v, ref.stored(v, err, "f32"), f"{k} of sequence {s}")
+    for k, (v, err) in sums.items():
+        ref.check(f64(g[k]), v, err + ref.TINY["f32"], k)
