@@ -172,7 +172,10 @@ __device__ void fill(const PlanArgs& a, const int32_t* starts, const int32_t* ti
         for (int i = 0; i < kPer; ++i) {
             const int64_t t = t0 + i;
             if (t < used) {
-                while (starts[s + 1] <= t) ++s;                 // (sequences without a token hold none)
+                if (starts[s + 1] <= t) {                       // the next sequence that has a token; any number may have none
+                    ++s;
+                    if (starts[s + 1] <= t) s = holder(starts, a.S, (int)t);
+                }
                 v[i] = s;
             } else {
                 v[i] = -1;

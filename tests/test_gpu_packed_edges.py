@@ -1,4 +1,4 @@
-"""Packed batches at the edges of their numbers: decays that overflow beside zeros."""
+"""Packed batches at the edges: decays that overflow beside zeros, decays of 0, tables that are mostly empty."""
 import numpy as np
 import pytest
 import torch
@@ -79,3 +79,27 @@ def test_states_that_keep_nothing(N, tile, value):
                 ref.check(f64(g[k][f:e]), v, ref.stored(v, err, "f32"), f"{k} of sequence {s}")
     for k, (v, err) in sums.items():
         ref.check(f64(g[k]), v, err + ref.TINY["f32"], k)
+
+
+# ------------------------------------------------------------------------------------------- the index
+@pytest.mark.parametrize("S", [3, 64, 4096, 4097, 131072])
+def test_plan_of_a_table_that_is_mostly_empty(S):
+    """A table of requests of which few have tokens: the empty entries between two of them are passed in one go, whatever their number."""
+    inside = [5] + [0] * (S - 3) + [1, 7]
+    behind = [5, 1, 7] + [0] * (S - 3)
+    took = []
+    for lengths in (inside, behind):
+        lens, T = ints(*lengths), 15
+        p = corey.corey_pack_plan(lens, T, 16)
+        for got, want, what in zip((p.starts, p.seq, p.tiles, p.blocks), ref.plan(lengths, T, 16), ("starts", "seq", "tiles", "blocks")):
+            assert np.array_equal(got.cpu().numpy(), want), what
+        times = []
+        for _ in range(5):
+            first, last = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            first.record()
+            corey.corey_pack_plan(lens, T, 16, table=p.table)
+            last.record()
+            torch.cuda.synchronize()
+            times.append(first.elapsed_time(last))
+        took.append(min(times))
+    assert took[0] < 3 * took[1] + 0.05, took                    # ms; one by one 131072 of them take 9, of 0.3 for the sums
