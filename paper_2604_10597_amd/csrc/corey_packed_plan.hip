@@ -144,6 +144,8 @@ __device__ __forceinline__ int holder(const int32_t* begin, int S, int i)
     return lo;
 }
 
+__device__ __forceinline__ int highest(int v) { return v > 0 ? 1 << (31 - __clz(v)) : 0; }    // the highest power of two in it
+
 __device__ void fill_pieces(const int32_t* starts, const int32_t* begin, int S, int size, Piece* out, int i, int room)
 {
     if (i >= room) return;
@@ -166,21 +168,28 @@ __device__ void fill(const PlanArgs& a, const int32_t* starts, const int32_t* ti
         const int64_t t0 = ((int64_t)g * kThreads + threadIdx.x) * kPer;
         if (t0 >= a.T) return;
         const int used = starts[a.S];
-        int s = holder(starts, a.S, (int)t0);
-        int v[kPer];
+        // Searches for the lane's first and last token side by side, then for those between them between the two: sequences without
+        // tokens may be any number there (passed one by one 131072 of them took 9 ms).
+        int v[kPer] = {};
+        for (int step = highest(a.S - 1); step > 0; step >>= 1) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int64_t t = t0 + i;
-            if (t < used) {
-                if (starts[s + 1] <= t) {                       // the next sequence that has a token; any number may have none
-                    ++s;
-                    if (starts[s + 1] <= t) s = holder(starts, a.S, (int)t);
-                }
-                v[i] = s;
-            } else {
-                v[i] = -1;
+            for (int i = 0; i < kPer; i += kPer - 1) {
+                const int s = min(v[i] + step, a.S - 1);
+                if (starts[s] <= t0 + i) v[i] = s;
             }
         }
+#pragma unroll
+        for (int i = 1; i < kPer - 1; ++i) v[i] = v[0];
+        for (int step = highest(v[kPer - 1] - v[0]); step > 0; step >>= 1) {
+#pragma unroll
+            for (int i = 1; i < kPer - 1; ++i) {
+                const int s = min(v[i] + step, v[kPer - 1]);
+                if (starts[s] <= t0 + i) v[i] = s;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t0 + i >= used) v[i] = -1;
         if (t0 + kPer <= a.T) {
             *reinterpret_cast<int4*>(a.seq + t0) = make_int4(v[0], v[1], v[2], v[3]);
         } else {
