@@ -242,7 +242,8 @@ struct StepArgs {
 // States in whole groups of four in aligned memory: U sets of 256 lanes a workgroup, every load of theirs issued before any use.  Bound by
 // memory (8 bytes a state).  One set, two and four, states from HBM, us, sequences of 5120 bf16 channels with 16 states: 16 (1280 sets)
 // 6.5, 6.7, 10; 40 12.2, 10.5, 13.7; 64 17.3, 14.6, 22; 512 115, 100, 132 (3.6 TB/s; a copy reaches 4.9); of 1536 channels 40 (960 sets) 5.6,
-// 5.7; 64 (1536) 7.0, 6.6; binary32, 5120: 16 6.3, 5.9; 64 17.3, 14.0; 512 110, 97.
+// 5.7; 64 (1536) 7.0, 6.6; binary32, 5120: 16 6.3, 5.9; 64 17.3, 14.0; 512 110, 97.  The line between one and two is that of 16-bit rows
+// (in binary32 two win by 0.4 us at 1280 sets already).
 constexpr uint64_t kManySets = 1400;
 template <typename T, int U>
 __global__ __launch_bounds__(256) void k_packed_step(StepArgs a)
